@@ -23,8 +23,12 @@ from .binding import (  # noqa: F401
     rrs_verify_tree,
     rrs_verify_tree_stats,
     set_row_split,
+    spechub_cache_accept,
+    spechub_cache_append,
     spechub_draft_sample,
     spechub_draft_sample_stats,
+    spechub_tree_attention,
+    spechub_tree_tables,
     spechub_verify_tree,
     spechub_verify_tree_stats,
     spechub_verify_tree_static,

@@ -29,6 +29,8 @@ STATUS_BITS = {
     "ZERO_RESIDUAL": 16,
     "INTERNAL": 32,
     "STATS": 64,
+    "PAGE": 128,
+    "PATH": 256,
 }
 
 
@@ -442,6 +444,58 @@ def spechub_verify_tree_static(target_logits, draft_logits, draft_tokens, unifor
     ``alloc_verify_outputs``) to keep this wrapper from allocating the result tensors too."""
     return (_native or _load_native()).verify_static(target_logits, draft_logits, draft_tokens, uniforms, tree,
                                                      temperature, stream, out, _split)
+
+
+# ---- scoring the tree with the target model: the paged cache (include/spechub_cache.h) -------------------------
+
+def spechub_tree_tables(tree: Tree, nodes: int, device="cuda"):
+    """What the cache operators want to know of a tree of ``nodes`` nodes: dict(depth, mask).  ``depth`` int32
+    [nodes] is a node's distance from the root, ``mask`` int32 [nodes][ceil(nodes / 32)] the nodes that it sees in
+    attention (its ancestors and itself) as bits.  A plan: made once per tree, on the host."""
+    if nodes < 1:
+        raise ValueError("a tree has at least one node")
+    child = None if tree.child is None else tree.child.cpu().tolist()
+    if child is not None and len(child) != nodes:
+        raise ValueError("child must be [nodes][k]")
+    words, depth = (nodes + 31) // 32, [0] * nodes
+    sees = [1 << n for n in range(nodes)]
+    for n in range(nodes):
+        for c in child[n] if child is not None else range(tree.k * n + 1, tree.k * n + 1 + tree.k):
+            if n < c < nodes:
+                depth[c] = depth[n] + 1
+                sees[c] |= sees[n]
+    rows = [[((s >> (32 * w)) & 0xFFFFFFFF) - ((s >> (32 * w + 31) & 1) << 32) for w in range(words)] for s in sees]
+    return dict(depth=torch.tensor(depth, dtype=torch.int32).to(device), mask=torch.tensor(rows, dtype=torch.int32).to(device))
+
+
+def spechub_cache_append(q, k, v, k_cache, v_cache, pages, lens, depth=None, inv_freq=None, pos_offset=0,
+                         interleaved=False, q_out=None, stream=None):
+    """Append the nodes' keys and values ([batch][nodes][kv_heads][head_dim]) behind the sequences' contexts in the
+    paged cache ([pages][page_size][kv_heads][head_dim], any strides), rotated by position on the way.  ``pages`` int32
+    [batch][pages per sequence], ``lens`` int32 [batch] (< 0: absent), ``depth`` from ``spechub_tree_tables`` (None: a
+    chunk of a prompt), ``inv_freq`` float32 [rotated / 2] (None: no rotation), ``pos_offset`` the length of a prefix that
+    the batch shares.  ``q`` ([batch][nodes][heads][head_dim] or None) is rotated into ``q_out`` (q itself is allowed; a
+    new tensor by default).  Returns dict(q, status)."""
+    return (_native or _load_native()).cache_append(q, k, v, k_cache, v_cache, pages, lens, depth, inv_freq, pos_offset,
+                                                    interleaved, q_out, stream)
+
+
+def spechub_tree_attention(q, k_cache, v_cache, pages, lens, mask, scale=None, shared_pages=None, shared_len=0, out=None,
+                           stream=None):
+    """Attention of every node to the ``shared_len`` tokens of ``shared_pages`` (int32, a prefix that the whole batch
+    shares: read once for all), to its sequence's own context and to the nodes that it sees (``mask`` from
+    ``spechub_tree_tables``, or one per sequence).  ``scale`` defaults to head_dim ** -0.5.  Pass ``out`` (a dict that a
+    former call returned) to reuse its tensors; rows of absent sequences are left as they were.  Returns dict(out, lse,
+    status)."""
+    return (_native or _load_native()).tree_attention(q, k_cache, v_cache, pages, lens, mask, scale, shared_pages,
+                                                      shared_len, out, stream)
+
+
+def spechub_cache_accept(k_cache, v_cache, pages, lens, path_nodes, nodes=None, stream=None):
+    """Move the cache entries of the accepted path (``path_nodes`` of a verify call) up to the end of the context, in all
+    layers of the cache ([layers][pages][page_size][kv_heads][head_dim], or one layer without the first axis).
+    ``nodes``: nodes of the tree, to refuse entries that are none.  Returns dict(lens, status) with the new lengths."""
+    return (_native or _load_native()).cache_accept(k_cache, v_cache, pages, lens, path_nodes, nodes, stream)
 
 
 def workspace_bytes(logits, tree: Tree, temperature=1.0) -> int:

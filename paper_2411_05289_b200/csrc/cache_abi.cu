@@ -1,0 +1,160 @@
+// C ABI of the cache operators (include/spechub_cache.h): host-side argument checks.
+#include <math.h>
+
+#include "spechub_cache.h"
+#include "spechub_cache_launch.h"
+
+namespace {
+
+using namespace spechub;
+
+int check_cache_desc(const spechub_cache_desc *d) {
+    if (!d) return SPECHUB_ERR_NULL;
+    if (d->struct_size != sizeof(spechub_cache_desc) || d->version != SPECHUB_ABI_VERSION) return SPECHUB_ERR_VERSION;
+    if (d->dtype != SPECHUB_BF16 && d->dtype != SPECHUB_F16) return SPECHUB_ERR_DTYPE;
+    if (d->batch < 0 || d->nodes < 1) return SPECHUB_ERR_SHAPE;
+    if (d->kv_heads < 1 || d->heads < d->kv_heads || d->heads % d->kv_heads != 0 || (d->head_dim != 64 && d->head_dim != 128) ||
+        d->page_size < 8 || d->page_size > 1024 || (d->page_size & (d->page_size - 1)) != 0 || d->pages < 1 || d->layers < 1 ||
+        d->table_width < 1)
+        return SPECHUB_ERR_CACHE;
+    if (static_cast<int64_t>(d->batch) * d->nodes > 0x7fffffffLL / d->heads) return SPECHUB_ERR_SHAPE;
+    // slots are counted in 32 bits where a sequence's keys are
+    if ((static_cast<int64_t>(d->table_width) + 1) * d->page_size > 0x7fffffffLL) return SPECHUB_ERR_CACHE;
+    if (d->batch > 1 && d->stride_table < d->table_width) return SPECHUB_ERR_STRIDE;
+    return SPECHUB_OK;
+}
+
+bool at16(const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+
+// A stride as the kernels take it: that of a dimension of size 1 is any.  `apart`: places of the dimension may not be the same.
+bool stride(int64_t s, int64_t count, int64_t least, bool apart, int64_t *out) {
+    *out = count > 1 ? s : least;
+    return count <= 1 || (s >= (apart ? least : 0) && s % 8 == 0);
+}
+
+int heads_of(const spechub_heads *x, const spechub_cache_desc *d, int heads, bool written, HeadsPtr *out) {
+    if (!x || !x->data) return SPECHUB_ERR_NULL;
+    out->data = x->data;
+    return at16(x->data) && stride(x->stride_seq, d->batch, d->head_dim, written, &out->seq) &&
+                   stride(x->stride_node, d->nodes, d->head_dim, written, &out->node) &&
+                   stride(x->stride_head, heads, d->head_dim, written, &out->head)
+               ? SPECHUB_OK
+               : SPECHUB_ERR_ALIGN;
+}
+
+int pages_of(const spechub_pages *x, const spechub_cache_desc *d, PagesPtr *out) {
+    if (!x || !x->data) return SPECHUB_ERR_NULL;
+    out->data = x->data;
+    return at16(x->data) && stride(x->stride_layer, d->layers, d->head_dim, true, &out->layer) &&
+                   stride(x->stride_page, d->pages, d->head_dim, true, &out->page) &&
+                   stride(x->stride_token, d->page_size, d->head_dim, true, &out->token) &&
+                   stride(x->stride_head, d->kv_heads, d->head_dim, true, &out->head)
+               ? SPECHUB_OK
+               : SPECHUB_ERR_ALIGN;
+}
+
+int cache_args(const spechub_cache_desc *d, const spechub_pages *k, const spechub_pages *v, uint32_t *status, CacheArgs *c) {
+    if (!d->table || !d->lens) return SPECHUB_ERR_NULL;
+    int rc = pages_of(k, d, &c->k);
+    if (rc == SPECHUB_OK) rc = pages_of(v, d, &c->v);
+    if (rc != SPECHUB_OK) return rc;
+    c->table = d->table;
+    c->lens = d->lens;
+    c->stride_table = d->batch > 1 ? d->stride_table : d->table_width;
+    c->batch = d->batch; c->nodes = d->nodes; c->heads = d->heads; c->kv_heads = d->kv_heads; c->head_dim = d->head_dim;
+    c->page_shift = __builtin_ctz(static_cast<unsigned>(d->page_size));
+    c->pages = d->pages; c->table_width = d->table_width; c->layers = d->layers;
+    c->status = status;
+    return SPECHUB_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int spechub_cache_append(const spechub_cache_desc *desc, const spechub_heads *q, const spechub_heads *k,
+                         const spechub_heads *v, const spechub_pages *k_cache, const spechub_pages *v_cache,
+                         const int32_t *depth, int64_t depth_stride_seq, const float *inv_freq, int32_t rotated,
+                         int32_t interleaved, int64_t pos_offset, const spechub_heads *q_out, uint32_t *status,
+                         void *stream) {
+    int rc = check_cache_desc(desc);
+    if (rc != SPECHUB_OK) return rc;
+    if (desc->layers != 1) return SPECHUB_ERR_CACHE;
+    if (rotated < 0 || rotated > desc->head_dim || rotated % 16 != 0 || (interleaved != 0 && interleaved != 1)) return SPECHUB_ERR_ROTARY;
+    if (depth_stride_seq < 0 || (depth_stride_seq != 0 && depth_stride_seq < desc->nodes)) return SPECHUB_ERR_STRIDE;
+    if (desc->batch == 0) return SPECHUB_OK;
+    AppendArgs a = {};
+    rc = cache_args(desc, k_cache, v_cache, status, &a.c);
+    if (rc == SPECHUB_OK) rc = heads_of(k, desc, desc->kv_heads, false, &a.k);
+    if (rc == SPECHUB_OK) rc = heads_of(v, desc, desc->kv_heads, false, &a.v);
+    if (rc == SPECHUB_OK && q) {
+        rc = heads_of(q, desc, desc->heads, false, &a.q);
+        if (rc == SPECHUB_OK) rc = heads_of(q_out, desc, desc->heads, true, &a.q_out);
+    }
+    if (rc != SPECHUB_OK) return rc;
+    if (rotated > 0 && !inv_freq) return SPECHUB_ERR_NULL;
+    a.depth = depth;
+    a.depth_stride_seq = depth_stride_seq;
+    a.inv_freq = inv_freq;
+    a.rotated = rotated;
+    a.pos_offset = pos_offset;
+    return launch_append(desc->dtype, a, interleaved == 1, static_cast<cudaStream_t>(stream));
+}
+
+size_t spechub_tree_attention_workspace_bytes(const spechub_cache_desc *desc, int64_t shared_len) {
+    if (check_cache_desc(desc) != SPECHUB_OK || shared_len < 0 || desc->batch == 0) return 0;
+    CacheArgs c = {};
+    c.batch = desc->batch; c.nodes = desc->nodes; c.heads = desc->heads; c.kv_heads = desc->kv_heads; c.head_dim = desc->head_dim;
+    return attention_workspace(c, shared_len);
+}
+
+int spechub_tree_attention(const spechub_cache_desc *desc, const spechub_heads *q, const spechub_pages *k_cache,
+                           const spechub_pages *v_cache, const int32_t *mask, int64_t mask_stride_seq,
+                           const int32_t *shared_table, int32_t shared_width, int64_t shared_len, float scale,
+                           const spechub_heads *out, float *lse, uint32_t *status, void *workspace,
+                           size_t workspace_bytes, void *stream) {
+    int rc = check_cache_desc(desc);
+    if (rc != SPECHUB_OK) return rc;
+    if (desc->layers != 1) return SPECHUB_ERR_CACHE;
+    if (!(scale > 0.f && isfinite(scale))) return SPECHUB_ERR_SCALE;
+    if (shared_len < 0 || shared_len > 0x3fffffffLL || shared_width < 0 || shared_len > static_cast<int64_t>(shared_width) * desc->page_size)
+        return SPECHUB_ERR_SHARED;
+    const int64_t words = (desc->nodes + 31) / 32;
+    if (mask_stride_seq < 0 || (mask_stride_seq != 0 && mask_stride_seq < words * desc->nodes)) return SPECHUB_ERR_STRIDE;
+    if (desc->batch == 0) return SPECHUB_OK;
+    AttentionArgs a = {};
+    rc = cache_args(desc, k_cache, v_cache, status, &a.c);
+    if (rc == SPECHUB_OK) rc = heads_of(q, desc, desc->heads, false, &a.q);
+    if (rc == SPECHUB_OK) rc = heads_of(out, desc, desc->heads, true, &a.out);
+    if (rc != SPECHUB_OK) return rc;
+    if (!mask || (shared_len > 0 && !shared_table)) return SPECHUB_ERR_NULL;
+    const size_t need = attention_workspace(a.c, shared_len);
+    if (workspace_bytes < need) return SPECHUB_ERR_WORKSPACE;
+    if (need && !workspace) return SPECHUB_ERR_NULL;
+    if (need && !at16(workspace)) return SPECHUB_ERR_ALIGN;
+    a.mask = mask;
+    a.mask_stride_seq = mask_stride_seq;
+    a.shared_table = shared_table;
+    a.shared_len = static_cast<int>(shared_len);
+    a.scale_log2 = scale * 1.4426950408889634f;
+    a.lse = lse;
+    return launch_attention(desc->dtype, a, workspace, static_cast<cudaStream_t>(stream));
+}
+
+int spechub_cache_accept(const spechub_cache_desc *desc, const spechub_pages *k_cache, const spechub_pages *v_cache,
+                         const int32_t *path_nodes, int32_t levels, int32_t *lens_out, uint32_t *status, void *stream) {
+    int rc = check_cache_desc(desc);
+    if (rc != SPECHUB_OK) return rc;
+    if (levels < 1) return SPECHUB_ERR_SHAPE;
+    if (desc->batch == 0) return SPECHUB_OK;
+    AcceptArgs a = {};
+    rc = cache_args(desc, k_cache, v_cache, status, &a.c);
+    if (rc != SPECHUB_OK) return rc;
+    if (!path_nodes || !lens_out || lens_out == desc->lens) return SPECHUB_ERR_NULL;
+    a.path = path_nodes;
+    a.levels = levels;
+    a.lens_out = lens_out;
+    return launch_accept(a, static_cast<cudaStream_t>(stream));
+}
+
+}  // extern "C"

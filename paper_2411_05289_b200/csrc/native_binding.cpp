@@ -7,6 +7,7 @@
 #include <ATen/core/Tensor.h>
 #include <ATen/cuda/EmptyTensor.h>
 #include <ATen/ops/empty.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -16,6 +17,7 @@
 #include <string>
 
 #include "spechub.h"
+#include "spechub_cache.h"
 
 namespace {
 
@@ -44,6 +46,7 @@ struct Names {  // interned attribute and key names
     PyObject *tokens, *hub, *prob, *status, *stats;
     PyObject *accept_idx, *token, *beta, *rate, *n_accepted, *n_emitted, *path_nodes, *path_tokens;
     PyObject *spechub, *rrs, *rrsw;
+    PyObject *q, *out, *lse, *lens;
 } N;
 
 // Without the interpreter's lock: other Python threads run while a call waits for a place in a full launch queue or for
@@ -557,6 +560,263 @@ PyObject *verify_static_impl(PyObject *const *a, Py_ssize_t n) {
     return out.release();
 }
 
+// ---- the cache operators (spechub_cache.h) -------------------------------------------------------
+// Strides are handed on as they are; what they and the pointers may be is the library's to check.
+
+// The calls run on the cache's device, whichever is current; by default on that device's current stream.
+void *stream_on(PyObject *stream, const at::Device &dev) {
+    return stream == Py_None ? c10::cuda::getCurrentCUDAStream(dev.index()).stream() : stream_of(stream);
+}
+
+struct Heads {   // [batch][nodes][heads][head_dim]
+    spechub_heads h;
+    explicit Heads(const Tensor &t) {
+        h.data = const_cast<void *>(t.const_data_ptr());
+        h.stride_seq = t.stride(0); h.stride_node = t.stride(1); h.stride_head = t.stride(2);
+    }
+};
+const Tensor &heads_tensor(PyObject *o, const char *msg, int64_t B, int64_t Nn, int64_t H, int64_t D, const Tensor &like) {
+    const Tensor &t = tensor(o, msg);
+    if (t.dim() != 4 || t.size(0) != B || t.size(1) != Nn || (H >= 0 && t.size(2) != H) || t.size(3) != D || t.stride(3) != 1 ||
+        t.scalar_type() != like.scalar_type() || t.device() != like.device())
+        value_error(msg);
+    return t;
+}
+
+struct Cache {
+    spechub_cache_desc d = {};
+    spechub_pages k, v;
+    int64_t B, D, Hk;
+    at::Device dev{at::kCPU};
+    const Tensor *kc;
+
+    // layered: [layers][pages][page_size][kv_heads][head_dim] is taken too
+    Cache(PyObject *ko, PyObject *vo, PyObject *table, PyObject *lens, bool layered) {
+        const char *msg = "k_cache and v_cache must be tensors [pages][page_size][kv_heads][head_dim] of one shape, with a contiguous last axis, bfloat16 or float16";
+        const Tensor &kt = tensor(ko, msg), &vt = tensor(vo, msg);
+        const auto st = kt.scalar_type();
+        if (!(kt.dim() == 4 || (layered && kt.dim() == 5)) || kt.sizes() != vt.sizes() || st != vt.scalar_type() ||
+            (st != at::kBFloat16 && st != at::kHalf) || kt.stride(-1) != 1 || vt.stride(-1) != 1 || vt.device() != kt.device())
+            value_error(msg);
+        if (!kt.is_cuda()) value_error("the cache must live on a CUDA device");
+        kc = &kt;
+        dev = kt.device();
+        const int64_t at = kt.dim() - 4;
+        for (int64_t i = 0; i < kt.dim(); ++i)
+            if (kt.size(i) > 0x7fffffffLL) value_error(msg);
+        Hk = kt.size(at + 2); D = kt.size(at + 3);
+        const Tensor &tt = tensor(table, "pages must be a tensor"), &lt = tensor(lens, "lens must be a tensor");
+        if (tt.scalar_type() != at::kInt || tt.dim() != 2 || tt.device() != dev || (tt.size(1) > 1 && tt.stride(1) != 1))
+            value_error("pages must be an int32 [batch][pages per sequence] tensor with contiguous rows on the cache's device");
+        B = tt.size(0);
+        if (lt.scalar_type() != at::kInt || lt.dim() != 1 || lt.size(0) != B || (B > 1 && lt.stride(0) != 1) || lt.device() != dev)
+            value_error("lens must be a contiguous int32 [batch] tensor on the cache's device");
+        if (tt.size(1) > 0x7fffffffLL || B > 0x7fffffffLL) value_error("pages is too large");
+        d.struct_size = sizeof d;
+        d.version = SPECHUB_ABI_VERSION;
+        d.dtype = st == at::kBFloat16 ? SPECHUB_BF16 : SPECHUB_F16;
+        d.batch = static_cast<int32_t>(B);
+        d.nodes = 1;
+        d.heads = d.kv_heads = static_cast<int32_t>(Hk);
+        d.head_dim = static_cast<int32_t>(D);
+        d.pages = static_cast<int32_t>(kt.size(at));
+        d.page_size = static_cast<int32_t>(kt.size(at + 1));
+        d.layers = at ? static_cast<int32_t>(kt.size(0)) : 1;
+        d.table_width = static_cast<int32_t>(tt.size(1));
+        d.stride_table = tt.stride(0);
+        d.table = static_cast<const int32_t *>(tt.const_data_ptr());
+        d.lens = static_cast<const int32_t *>(lt.const_data_ptr());
+        for (int i = 0; i < 2; ++i) {
+            const Tensor &t = i ? vt : kt;
+            spechub_pages &p = i ? v : k;
+            p.data = const_cast<void *>(t.const_data_ptr());
+            p.stride_layer = at ? t.stride(0) : 0;
+            p.stride_page = t.stride(at); p.stride_token = t.stride(at + 1); p.stride_head = t.stride(at + 2);
+        }
+    }
+    void nodes(int64_t Nn, int64_t H) {
+        if (Nn > 0x7fffffffLL || H > 0x7fffffffLL) value_error("too many nodes or heads");
+        d.nodes = static_cast<int32_t>(Nn);
+        d.heads = static_cast<int32_t>(H);
+    }
+};
+
+// int32 [rest...] for all sequences or [batch][rest...]; the stride between sequences in words
+const int32_t *per_tree(PyObject *o, const Cache &c, at::IntArrayRef rest, const char *msg, int64_t *stride) {
+    const Tensor &t = tensor(o, msg);
+    const int64_t lead = t.dim() - static_cast<int64_t>(rest.size());
+    if (t.scalar_type() != at::kInt || !t.is_contiguous() || t.device() != c.dev || (lead != 0 && lead != 1) ||
+        t.sizes().slice(lead) != rest || (lead == 1 && t.size(0) != c.B))
+        value_error(msg);
+    int64_t n = 1;
+    for (const int64_t r : rest) n *= r;
+    *stride = lead == 1 ? n : 0;
+    return static_cast<const int32_t *>(t.const_data_ptr());
+}
+
+// (q, k, v, k_cache, v_cache, pages, lens, depth, inv_freq, pos_offset, interleaved, q_out, stream)
+PyObject *append_impl(PyObject *const *a, Py_ssize_t n) {
+    need_args(n, 13);
+    Cache c(a[3], a[4], a[5], a[6], false);
+    const char *msg = "q, k and v must be [batch][nodes][heads][head_dim] tensors of the cache's dtype, device and head size (k and v: and heads) with a contiguous last axis";
+    const Tensor &k0 = tensor(a[1], msg);
+    if (k0.dim() != 4) value_error(msg);
+    const int64_t Nn = k0.size(1);
+    const Tensor &k = heads_tensor(a[1], msg, c.B, Nn, c.Hk, c.D, *c.kc), &v = heads_tensor(a[2], msg, c.B, Nn, c.Hk, c.D, *c.kc);
+    const bool with_q = a[0] != Py_None;
+    Tensor q, qo;
+    if (with_q) {
+        q = heads_tensor(a[0], msg, c.B, Nn, -1, c.D, *c.kc);
+        if (a[11] != Py_None)
+            qo = heads_tensor(a[11], "q_out must be a tensor of q's shape, dtype and device with a contiguous last axis", c.B, Nn, q.size(2), c.D, *c.kc);
+    }
+    c.nodes(Nn, with_q ? q.size(2) : c.Hk);
+    const int32_t *depth = nullptr;
+    int64_t depth_stride = 0;
+    if (a[7] != Py_None)
+        depth = per_tree(a[7], c, {Nn}, "depth must be a contiguous int32 [nodes] or [batch][nodes] tensor on the cache's device", &depth_stride);
+    const float *freq = nullptr;
+    int64_t rotated = 0;
+    if (a[8] != Py_None) {
+        const char *fm = "inv_freq must be a contiguous float32 tensor of one axis, at most half a head long, on the cache's device";
+        const Tensor &f = tensor(a[8], fm);
+        if (f.scalar_type() != at::kFloat || f.dim() != 1 || !f.is_contiguous() || f.device() != c.dev || 2 * f.size(0) > c.D) value_error(fm);
+        freq = f.const_data_ptr<float>();
+        rotated = 2 * f.size(0);
+    }
+    const long long offset = PyLong_AsLongLong(a[9]);
+    if (PyErr_Occurred()) fail();
+    const bool next = truth(a[10]);
+    void *s = stream_on(a[12], c.dev);
+    const c10::cuda::CUDAGuard guard(c.dev);
+    const Heads hk(k), hv(v);
+    Tensor status;
+    int rc;
+    {
+        Unlocked u;
+        status = make({c.B}, at::kInt, c.dev);
+        if (with_q && !qo.defined()) qo = make({c.B, Nn, q.size(2), c.D}, c.kc->scalar_type(), c.dev);
+        const Heads hq(with_q ? q : k), ho(with_q ? qo : k);
+        rc = spechub_cache_append(&c.d, with_q ? &hq.h : nullptr, &hk.h, &hv.h, &c.k, &c.v, depth, depth_stride, freq,
+                                  static_cast<int32_t>(rotated), next, offset, with_q ? &ho.h : nullptr,
+                                  static_cast<uint32_t *>(status.data_ptr()), s);
+    }
+    check(rc);
+    Ref out(PyDict_New());
+    if (!out.o) fail();
+    if (with_q) put(out.o, N.q, qo);
+    put(out.o, N.status, status);
+    hold_values(a[12], out.o);
+    return out.release();
+}
+
+// (q, k_cache, v_cache, pages, lens, mask, scale, shared_pages, shared_len, out, stream)
+PyObject *attention_impl(PyObject *const *a, Py_ssize_t n) {
+    need_args(n, 11);
+    Cache c(a[1], a[2], a[3], a[4], false);
+    const char *msg = "q must be a [batch][nodes][heads][head_dim] tensor of the cache's dtype, device and head size with a contiguous last axis";
+    const Tensor &q0 = tensor(a[0], msg);
+    if (q0.dim() != 4) value_error(msg);
+    const int64_t Nn = q0.size(1), H = q0.size(2);
+    const Tensor &q = heads_tensor(a[0], msg, c.B, Nn, H, c.D, *c.kc);
+    c.nodes(Nn, H);
+    int64_t mask_stride;
+    const int32_t *mask = per_tree(a[5], c, {Nn, (Nn + 31) / 32},
+                                   "mask must be a contiguous int32 [nodes][ceil(nodes / 32)] tensor, or one of these per sequence, on the cache's device", &mask_stride);
+    double scale = 1.0 / std::sqrt(static_cast<double>(c.D > 0 ? c.D : 1));
+    if (a[6] != Py_None) {
+        const Ref f(PyNumber_Float(a[6]));
+        if (!f.o) fail();
+        scale = PyFloat_AS_DOUBLE(f.o);
+    }
+    const int32_t *shared = nullptr;
+    int64_t width = 0;
+    if (a[7] != Py_None) {
+        const char *sm = "shared_pages must be a contiguous int32 tensor of one axis on the cache's device";
+        const Tensor &t = tensor(a[7], sm);
+        if (t.scalar_type() != at::kInt || t.dim() != 1 || !t.is_contiguous() || t.device() != c.dev || t.size(0) > 0x7fffffffLL) value_error(sm);
+        shared = static_cast<const int32_t *>(t.const_data_ptr());
+        width = t.size(0);
+    }
+    const long long shared_len = PyLong_AsLongLong(a[8]);
+    if (PyErr_Occurred()) fail();
+    void *s = stream_on(a[10], c.dev);
+    const c10::cuda::CUDAGuard guard(c.dev);
+    Tensor out, lse, status, ws;
+    PyObject *const given = a[9];
+    if (given != Py_None) {
+        const char *om = "out must be a dict of tensors: out like q, lse a contiguous float32 [batch][nodes][heads], status a contiguous int32 [batch]";
+        Ref o(PyObject_GetItem(given, N.out)), l(PyObject_GetItem(given, N.lse)), st(PyObject_GetItem(given, N.status));
+        if (!o.o || !l.o || !st.o) fail();
+        out = heads_tensor(o.o, om, c.B, Nn, H, c.D, *c.kc);
+        lse = tensor(l.o, om);
+        status = tensor(st.o, om);
+        if (lse.scalar_type() != at::kFloat || !lse.is_contiguous() || lse.dim() != 3 || lse.size(0) != c.B || lse.size(1) != Nn ||
+            lse.size(2) != H || lse.device() != c.dev || status.scalar_type() != at::kInt || !status.is_contiguous() ||
+            status.dim() != 1 || status.size(0) != c.B || status.device() != c.dev)
+            value_error(om);
+    }
+    const Heads hq(q);
+    int rc;
+    {
+        Unlocked u;
+        if (given == Py_None) {
+            out = make({c.B, Nn, H, c.D}, c.kc->scalar_type(), c.dev);
+            lse = make({c.B, Nn, H}, at::kFloat, c.dev);
+            status = make({c.B}, at::kInt, c.dev);
+        }
+        const size_t bytes = spechub_tree_attention_workspace_bytes(&c.d, shared_len);
+        if (bytes) ws = make({static_cast<int64_t>(bytes)}, at::kByte, c.dev);
+        const Heads ho(out);
+        rc = spechub_tree_attention(&c.d, &hq.h, &c.k, &c.v, mask, mask_stride, shared, static_cast<int32_t>(width), shared_len,
+                                    static_cast<float>(scale), &ho.h, lse.data_ptr<float>(), static_cast<uint32_t *>(status.data_ptr()),
+                                    bytes ? ws.data_ptr() : nullptr, bytes, s);
+    }
+    check(rc);
+    Ref r(PyDict_New());
+    if (!r.o) fail();
+    put(r.o, N.out, out);
+    put(r.o, N.lse, lse);
+    put(r.o, N.status, status);
+    hold(a[10], ws);
+    hold_values(a[10], r.o);
+    return r.release();
+}
+
+// (k_cache, v_cache, pages, lens, path_nodes, nodes, stream)
+PyObject *accept_impl(PyObject *const *a, Py_ssize_t n) {
+    need_args(n, 7);
+    Cache c(a[0], a[1], a[2], a[3], true);
+    const char *msg = "path_nodes must be a contiguous int32 [batch][levels] tensor on the cache's device";
+    const Tensor &p = tensor(a[4], msg);
+    if (p.scalar_type() != at::kInt || p.dim() != 2 || p.size(0) != c.B || !p.is_contiguous() || p.device() != c.dev || p.size(1) > 0x7fffffffLL)
+        value_error(msg);
+    int64_t nodes = 0x7fffffffLL / (c.Hk > 0 ? c.Hk : 1) / (c.B > 0 ? c.B : 1);   // no limit given: what the library counts
+    if (a[5] != Py_None) {
+        nodes = PyLong_AsLongLong(a[5]);
+        if (PyErr_Occurred()) fail();
+    }
+    c.nodes(nodes, c.Hk);
+    void *s = stream_on(a[6], c.dev);
+    const c10::cuda::CUDAGuard guard(c.dev);
+    Tensor lens, status;
+    int rc;
+    {
+        Unlocked u;
+        lens = make({c.B}, at::kInt, c.dev);
+        status = make({c.B}, at::kInt, c.dev);
+        rc = spechub_cache_accept(&c.d, &c.k, &c.v, static_cast<const int32_t *>(p.const_data_ptr()), static_cast<int32_t>(p.size(1)),
+                                  static_cast<int32_t *>(lens.data_ptr()), static_cast<uint32_t *>(status.data_ptr()), s);
+    }
+    check(rc);
+    Ref out(PyDict_New());
+    if (!out.o) fail();
+    put(out.o, N.lens, lens);
+    put(out.o, N.status, status);
+    hold_values(a[6], out.o);
+    return out.release();
+}
+
 template <PyObject *(*IMPL)(PyObject *const *, Py_ssize_t)>
 PyObject *guarded(PyObject *, PyObject *const *a, Py_ssize_t n) {
     try {
@@ -582,6 +842,9 @@ PyMethodDef methods[] = {
     FAST("compare_draft", compare_draft_impl),
     FAST("compare_verify", compare_verify_impl),
     FAST("verify_static", verify_static_impl),
+    FAST("cache_append", append_impl),
+    FAST("tree_attention", attention_impl),
+    FAST("cache_accept", accept_impl),
     {"set_error", set_error, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
@@ -597,6 +860,7 @@ PyMODINIT_FUNC PyInit__spechub_native() {
         {&N.accept_idx, "accept_idx"}, {&N.token, "token"}, {&N.beta, "beta"}, {&N.rate, "rate"},
         {&N.n_accepted, "n_accepted"}, {&N.n_emitted, "n_emitted"}, {&N.path_nodes, "path_nodes"}, {&N.path_tokens, "path_tokens"},
         {&N.spechub, "spechub"}, {&N.rrs, "rrs"}, {&N.rrsw, "rrsw"},
+        {&N.q, "q"}, {&N.out, "out"}, {&N.lse, "lse"}, {&N.lens, "lens"},
     };
     for (const auto &p : names)
         if (!(*p.first = PyUnicode_InternFromString(p.second))) return nullptr;

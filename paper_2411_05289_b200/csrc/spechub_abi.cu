@@ -7,6 +7,7 @@
 #include <mutex>
 
 #include "spechub.h"
+#include "spechub_cache.h"
 #include "spechub_launch.h"
 
 extern "C" size_t spechub_draft_stats_bytes(const spechub_desc *desc);
@@ -632,12 +633,17 @@ const char *spechub_status_string(int code) {
         case SPECHUB_ERR_NULL: return "a required pointer is NULL";
         case SPECHUB_ERR_VERSION: return "descriptor struct_size/version mismatch";
         case SPECHUB_ERR_SHAPE: return "bad shape: need batch >= 0, nodes >= 1, vocab >= 2, 2 <= k <= 8 (k == 2 for SpecHub), levels >= 1, valid flags";
-        case SPECHUB_ERR_DTYPE: return "dtype must be SPECHUB_F32 or SPECHUB_BF16";
+        case SPECHUB_ERR_DTYPE: return "dtype must be SPECHUB_F32 or SPECHUB_BF16 (the cache operators: SPECHUB_BF16 or SPECHUB_F16)";
         case SPECHUB_ERR_STRIDE: return "strides too small for the given shape";
         case SPECHUB_ERR_TEMPERATURE: return "temperature must be finite and > 0";
         case SPECHUB_ERR_WORKSPACE: return "workspace smaller than spechub_workspace_bytes()";
         case SPECHUB_ERR_LAUNCH: return "kernel launch failed";
         case SPECHUB_ERR_METHOD: return "without_replacement must be 0 or 1";
+        case SPECHUB_ERR_ALIGN: return "pointers and strides must be multiples of 16 bytes, rows that are written apart from each other";
+        case SPECHUB_ERR_CACHE: return "bad cache: need heads a multiple of kv_heads >= 1, head_dim 64 or 128, page_size a power of two from 8 to 1024, pages >= 1, table_width >= 1, layers >= 1 (1 but for accept)";
+        case SPECHUB_ERR_ROTARY: return "rotated must be a multiple of 16 from 0 to head_dim, interleaved 0 or 1";
+        case SPECHUB_ERR_SHARED: return "shared_len must be >= 0 and fit into the shared pages";
+        case SPECHUB_ERR_SCALE: return "scale must be finite and > 0";
         case SPECHUB_ERR_TOO_LARGE: return "batch * nodes exceeds SPECHUB_STATIC_MAX_ROWS of spechub_verify_tree_static";
         default: return "unknown status";
     }

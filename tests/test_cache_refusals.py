@@ -1,0 +1,200 @@
+"""The cache operators' host side: tree tables, descriptor layout, what is refused before any launch (no GPU needed)."""
+import ctypes
+import os
+import re
+
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import paper_2411_05289_b200 as sh  # noqa: E402
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+class Desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_uint32) for n in ("struct_size", "version")] + [
+        (n, ctypes.c_int32) for n in ("dtype", "batch", "nodes", "heads", "kv_heads", "head_dim", "page_size", "pages",
+                                      "layers", "table_width")] + [
+        ("stride_table", ctypes.c_int64), ("table", ctypes.c_void_p), ("lens", ctypes.c_void_p)]
+
+
+class Pages(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p)] + [(n, ctypes.c_int64) for n in ("layer", "page", "token", "head")]
+
+
+class Heads(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p)] + [(n, ctypes.c_int64) for n in ("seq", "node", "head")]
+
+
+def desc(**kw):
+    d = Desc(ctypes.sizeof(Desc), 1, 1, 2, 3, 8, 4, 64, 16, 10, 1, 5, 5, 4096, 4096)
+    for k, v in kw.items():
+        setattr(d, k, v)
+    return d
+
+
+def pages(**kw):
+    p = Pages(4096, 0, 16 * 4 * 64, 4 * 64, 64)
+    for k, v in kw.items():
+        setattr(p, k, v)
+    return p
+
+
+def heads(**kw):
+    p = Heads(4096, 3 * 8 * 64, 8 * 64, 64)
+    for k, v in kw.items():
+        setattr(p, k, v)
+    return p
+
+
+FAKE = ctypes.c_void_p(4096)   # never followed: every call below is refused on the host or has nothing to do
+ref = lambda x: None if x is None else ctypes.byref(x)  # noqa: E731
+
+
+def append(d=None, q=True, k=None, v=None, kc=None, vc=None, depth=None, depth_stride=0, freq=FAKE, rotated=64, interleaved=0,
+           qo=True, offset=0):
+    lib = sh.load_library()
+    new = lambda x: heads() if x is True else x  # noqa: E731
+    return lib.spechub_cache_append(ref(d or desc()), ref(new(q)), ref(k or heads()), ref(v or heads()), ref(kc or pages()),
+                                    ref(vc or pages()), depth, ctypes.c_int64(depth_stride), freq, rotated, interleaved,
+                                    ctypes.c_int64(offset), ref(new(qo)), None, None)
+
+
+def attend(d=None, q=None, kc=None, vc=None, mask=FAKE, mask_stride=0, shared=None, width=0, shared_len=0, scale=0.1,
+           out=None, workspace=FAKE, nbytes=1 << 40):
+    lib = sh.load_library()
+    return lib.spechub_tree_attention(ref(d or desc()), ref(q or heads()), ref(kc or pages()), ref(vc or pages()), mask,
+                                      ctypes.c_int64(mask_stride), shared, width, ctypes.c_int64(shared_len), ctypes.c_float(scale),
+                                      ref(out or heads()), None, None, workspace, ctypes.c_size_t(nbytes), None)
+
+
+def accept(d=None, kc=None, vc=None, path=FAKE, levels=3, lens_out=ctypes.c_void_p(8192)):
+    lib = sh.load_library()
+    return lib.spechub_cache_accept(ref(d or desc()), ref(kc or pages()), ref(vc or pages()), path, levels, lens_out, None, None)
+
+
+def test_every_declared_function_is_exported():
+    src = re.sub(r"/\*.*?\*/", "", open(os.path.join(ROOT, "include", "spechub_cache.h")).read(), flags=re.S)
+    names = set(re.findall(r"\b(spechub_[a-z_]+)\s*\(", src))
+    assert names == {"spechub_cache_append", "spechub_tree_attention", "spechub_tree_attention_workspace_bytes", "spechub_cache_accept"}
+    for n in names:
+        assert hasattr(sh.load_library(), n)
+
+
+BAD_DESC = [(dict(struct_size=8), -2), (dict(version=2), -2), (dict(dtype=0), -4), (dict(dtype=3), -4), (dict(batch=-1), -3),
+            (dict(nodes=0), -3), (dict(kv_heads=0), -12), (dict(heads=6), -12), (dict(heads=2), -12), (dict(head_dim=96), -12),
+            (dict(page_size=4), -12), (dict(page_size=24), -12), (dict(page_size=2048), -12), (dict(pages=0), -12),
+            (dict(layers=0), -12), (dict(table_width=0), -12), (dict(stride_table=4), -5), (dict(batch=1 << 30, nodes=1 << 10), -3),
+            (dict(table_width=1 << 28, stride_table=1 << 28, page_size=64), -12), (dict(table=None), -1), (dict(lens=None), -1)]
+
+
+@pytest.mark.parametrize("change,code", BAD_DESC)
+def test_bad_descriptors_are_refused(change, code):
+    for call in (append, attend, accept):
+        assert call(desc(**change)) == code, (call.__name__, change)
+
+
+@pytest.mark.parametrize("change", [dict(data=4104), dict(page=16 * 4 * 64 + 4), dict(token=20), dict(head=68), dict(head=0), dict(token=-64)])
+def test_misplaced_caches_are_refused(change):
+    for call in (append, attend, accept):
+        assert call(kc=pages(**change)) == -11 and call(vc=pages(**change)) == -11
+        assert call(kc=pages(data=None)) == -1
+
+
+def test_append_refuses():
+    for bad in (dict(data=4098), dict(seq=1001), dict(node=4), dict(head=-8)):
+        assert append(k=heads(**bad)) == -11 and append(v=heads(**bad)) == -11
+        assert append(q=heads(**bad)) == -11 and append(qo=heads(**bad)) == -11
+    assert append(qo=heads(head=0)) == -11       # rows that are written may not lie over each other
+    assert append(qo=None) == -1
+    for rotated in (-16, 8, 72, 80, 128):
+        assert append(rotated=rotated) == -13
+    assert append(interleaved=2) == -13
+    assert append(freq=None) == -1
+    assert append(depth=FAKE, depth_stride=2) == -5
+    assert append(desc(layers=2)) == -12
+    assert append(desc(batch=0)) == 0
+
+
+def test_attention_refuses():
+    assert attend(q=heads(node=4)) == -11 and attend(out=heads(data=4100)) == -11 and attend(out=heads(seq=0)) == -11
+    for scale in (0.0, -1.0, float("nan"), float("inf")):
+        assert attend(scale=scale) == -15
+    assert attend(shared=FAKE, width=2, shared_len=33) == -14
+    assert attend(shared=FAKE, width=2, shared_len=-1) == -14
+    assert attend(shared=None, width=2, shared_len=32) == -1
+    assert attend(mask=None) == -1
+    assert attend(mask_stride=2) == -5
+    assert attend(desc(layers=2)) == -12
+    lib = sh.load_library()
+    lib.spechub_tree_attention_workspace_bytes.restype = ctypes.c_size_t
+    need = lib.spechub_tree_attention_workspace_bytes(ref(desc()), ctypes.c_int64(0))
+    if need:
+        assert attend(nbytes=need - 1) == -7
+        assert attend(workspace=None) == -1
+        assert attend(workspace=ctypes.c_void_p(4104)) == -11
+    assert attend(desc(batch=0)) == 0
+    assert lib.spechub_tree_attention_workspace_bytes(ref(desc(nodes=0)), ctypes.c_int64(0)) == 0
+
+
+def test_accept_refuses():
+    assert accept(levels=0) == -3
+    assert accept(path=None) == -1 and accept(lens_out=None) == -1
+    assert accept(lens_out=ctypes.c_void_p(4096)) == -1   # the lengths themselves
+    assert accept(desc(batch=0)) == 0
+
+
+def test_status_strings():
+    for code, word in ((-11, "16 bytes"), (-12, "head_dim"), (-13, "rotated"), (-14, "shared"), (-15, "scale")):
+        assert word in sh.status_string(code)
+
+
+def brute(parents):
+    n = len(parents)
+    sees = np.eye(n, dtype=bool)
+    for i in range(n):
+        j = parents[i]
+        while j >= 0:
+            sees[i, j] = True
+            j = parents[j]
+    return sees
+
+
+def as_bits(mask, n):
+    words = mask.numpy().view(np.uint32)
+    return np.array([[bool(words[i, j // 32] >> (j % 32) & 1) for j in range(32 * words.shape[1])] for i in range(n)])
+
+
+@pytest.mark.parametrize("k,n", [(1, 1), (1, 40), (2, 1), (2, 7), (2, 31), (3, 13), (2, 63), (4, 100)])
+def test_tables_of_complete_trees(k, n):
+    t = sh.spechub_tree_tables(sh.Tree(levels=1, k=k), n, device="cpu")
+    parents = [-1] + [(i - 1) // k for i in range(1, n)]
+    bits = as_bits(t["mask"], n)
+    np.testing.assert_array_equal(bits[:, :n], brute(parents))
+    assert not bits[:, n:].any()
+    np.testing.assert_array_equal(t["depth"].numpy(), brute(parents).sum(1) - 1)
+
+
+def test_tables_of_a_listed_tree():
+    parents = [-1, 0, 0, 1, 1, 2, 3]
+    t = sh.spechub_tree_tables(sh.Tree.from_parents(parents, device="cpu"), 7, device="cpu")
+    np.testing.assert_array_equal(as_bits(t["mask"], 7)[:, :7], brute(parents))
+    with pytest.raises(ValueError):
+        sh.spechub_tree_tables(sh.Tree.from_parents(parents, device="cpu"), 8, device="cpu")
+    with pytest.raises(ValueError):
+        sh.spechub_tree_tables(sh.Tree.heap(7), 0, device="cpu")
+
+
+def test_tensors_off_the_device_are_refused():
+    z = torch.zeros((4, 8, 1, 64), dtype=torch.bfloat16)
+    one = torch.zeros((1, 1), dtype=torch.int32)
+    with pytest.raises(ValueError):
+        sh.spechub_cache_accept(z, z, one, one[0], one)
+    with pytest.raises(ValueError):
+        sh.spechub_tree_attention(z, z, z, one, one[0], one)
+    with pytest.raises(ValueError):
+        sh.spechub_cache_append(z, z, z, z, z, one, one[0])
+    with pytest.raises(TypeError):
+        sh.spechub_cache_accept(None, z, one, one[0], one)
