@@ -105,6 +105,7 @@ size_t spechub_tree_attention_workspace_bytes(const spechub_cache_desc *desc, in
     if (check_cache_desc(desc) != SPECHUB_OK || shared_len < 0 || desc->batch == 0) return 0;
     CacheArgs c = {};
     c.batch = desc->batch; c.nodes = desc->nodes; c.heads = desc->heads; c.kv_heads = desc->kv_heads; c.head_dim = desc->head_dim;
+    c.page_shift = __builtin_ctz(static_cast<unsigned>(desc->page_size)); c.table_width = desc->table_width;
     return attention_workspace(c, shared_len);
 }
 

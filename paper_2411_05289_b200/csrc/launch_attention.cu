@@ -1,23 +1,105 @@
-// Attention of tree nodes over a paged cache.
+// Attention of tree nodes over a paged cache: tensor maps, workspace, launches.
+#include <mutex>
+
 #include "spechub_attention.cuh"
 #include "spechub_cache_launch.h"
+#include "spechub_shapes.h"
 
 namespace spechub {
 
-template <class T>
-static int launch_rows(const AttentionArgs &a, cudaStream_t s) {
-    const int64_t rows = int64_t(a.c.batch) * a.c.nodes * a.c.heads, per = kAttRowThreads / 32;
-    const unsigned grid = static_cast<unsigned>((rows + per - 1) / per);
-    return a.c.head_dim == 64 ? launch_grid(attention_rows_kernel<T, 64>, grid, kAttRowThreads, 0, 1, s, a)
-                              : launch_grid(attention_rows_kernel<T, 128>, grid, kAttRowThreads, 0, 1, s, a);
+namespace {
+
+using Encode = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
+                            const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+Encode encoder() {
+    static std::mutex mutex;
+    static Encode found = nullptr;
+    std::lock_guard<std::mutex> lock(mutex);
+    if (!found) {
+        void *f = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &q) != cudaSuccess || q != cudaDriverEntryPointSuccess) {
+            cudaGetLastError();
+            return nullptr;
+        }
+        found = reinterpret_cast<Encode>(f);
+    }
+    return found;
 }
 
-size_t attention_workspace(const CacheArgs &, int64_t) { return 0; }
+// (head_dim, token of a page, head, page), boxes of 64 dimensions of a page's tokens (128 of them at most)
+int page_map(int dtype, const PagesPtr &x, const CacheArgs &c, CUtensorMap *map) {
+    const Encode encode = encoder();
+    if (!encode) return SPECHUB_ERR_LAUNCH;
+    const cuuint32_t ps = 1u << c.page_shift;
+    const cuuint64_t dims[4] = {static_cast<cuuint64_t>(c.head_dim), ps, static_cast<cuuint64_t>(c.kv_heads), static_cast<cuuint64_t>(c.pages)};
+    const cuuint64_t strides[3] = {static_cast<cuuint64_t>(x.token) * 2, static_cast<cuuint64_t>(x.head) * 2, static_cast<cuuint64_t>(x.page) * 2};
+    const cuuint32_t box[4] = {64, ps < kTile ? ps : kTile, 1, 1}, each[4] = {1, 1, 1, 1};
+    const CUresult r = encode(map, dtype == SPECHUB_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, x.data, dims, strides, box,
+                              each, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? SPECHUB_OK : SPECHUB_ERR_ALIGN;
+}
 
-int launch_attention(int dtype, const AttentionArgs &a, void *, cudaStream_t s) {
-    const int rc = dtype == SPECHUB_BF16 ? launch_rows<__nv_bfloat16>(a, s) : launch_rows<__half>(a, s);
-    if (rc != SPECHUB_OK || !a.c.status) return rc;
-    return launch_grid(attention_status_kernel, a.c.batch, kAttStatusThreads, 0, 1, s, a);
+size_t up(size_t n) { return (n + 255) & ~size_t(255); }
+
+// The plan, and the workspace's size; its parts are at `base`.
+size_t plan_of(const CacheArgs &c, int64_t shared_len, uint8_t *base, AttPlan *p) {
+    const int64_t own = static_cast<int64_t>(c.nodes) * (c.heads / c.kv_heads), all = own * c.batch;
+    p->shared_tiles = static_cast<int>((shared_len + kTile - 1) / kTile);
+    p->shared_blocks = shared_len ? static_cast<int>((all + kBlockRows - 1) / kBlockRows) : 0;
+    p->own_blocks = static_cast<int>((own + kBlockRows - 1) / kBlockRows);
+    p->shared_rows = static_cast<int>(all < kBlockRows ? all : kBlockRows);
+    p->own_rows = static_cast<int>(own < kBlockRows ? own : kBlockRows);
+    p->shared_items = static_cast<int64_t>(c.kv_heads) * p->shared_blocks;
+    p->shared_units = p->shared_items * p->shared_tiles;
+    // as many CTAs as there can be units, at most one per SM
+    const int64_t own_items = static_cast<int64_t>(c.batch) * c.kv_heads * p->own_blocks;
+    const int64_t most = p->shared_units + own_items * (((static_cast<int64_t>(c.table_width) << c.page_shift) + kTile - 1) / kTile);
+    p->grid = static_cast<int>(most < kSms ? most : kSms);
+    p->slots = shared_len ? p->shared_items + p->grid : 0;
+    const int64_t rows = p->slots * p->shared_rows + (own_items + p->grid) * p->own_rows;
+    size_t at = 0;
+    p->before = reinterpret_cast<int64_t *>(base);
+    at += up(sizeof(int64_t) * (static_cast<size_t>(c.batch) + 1));
+    p->error = reinterpret_cast<int *>(base + at);
+    at += up(sizeof(int) * static_cast<size_t>(p->grid));
+    p->ml = reinterpret_cast<float2 *>(base + at);
+    at += up(sizeof(float2) * static_cast<size_t>(rows));
+    p->o = reinterpret_cast<float *>(base + at);
+    return at + up(sizeof(float) * static_cast<size_t>(rows) * c.head_dim);
+}
+
+template <class T, int D>
+int launch_type(const AttKernelArgs &k, const CUtensorMap &mk, const CUtensorMap &mv, cudaStream_t s) {
+    static bool configured[kMaxDevices] = {};
+    const int rc = allow_smem(reinterpret_cast<const void *>(attention_kernel<T, D>), AttShape<D>::kSmem, configured);
+    if (rc != SPECHUB_OK) return rc;
+    const int lrc = launch_grid(attention_kernel<T, D>, k.p.grid, kAttThreads, AttShape<D>::kSmem, 1, s, k, mk, mv);
+    if (lrc != SPECHUB_OK) return lrc;
+    const int64_t rows = static_cast<int64_t>(k.a.c.batch) * k.a.c.nodes * k.a.c.heads, per = kJoinThreads / 32;
+    const unsigned grid = static_cast<unsigned>((rows + per - 1) / per + (k.a.c.status ? k.a.c.batch : 0));
+    return launch_grid(attention_join_kernel<T, D>, grid, kJoinThreads, 0, 1, s, k);
+}
+
+}  // namespace
+
+size_t attention_workspace(const CacheArgs &c, int64_t shared_len) {
+    AttPlan p;
+    return plan_of(c, shared_len, nullptr, &p);
+}
+
+int launch_attention(int dtype, const AttentionArgs &a, void *workspace, cudaStream_t s) {
+    AttKernelArgs k;
+    k.a = a;
+    plan_of(a.c, a.shared_len, static_cast<uint8_t *>(workspace), &k.p);
+    CUtensorMap mk, mv;
+    int rc = page_map(dtype, a.c.k, a.c, &mk);
+    if (rc == SPECHUB_OK) rc = page_map(dtype, a.c.v, a.c, &mv);
+    if (rc != SPECHUB_OK) return rc;
+    if (dtype == SPECHUB_BF16) return a.c.head_dim == 64 ? launch_type<__nv_bfloat16, 64>(k, mk, mv, s) : launch_type<__nv_bfloat16, 128>(k, mk, mv, s);
+    return a.c.head_dim == 64 ? launch_type<__half, 64>(k, mk, mv, s) : launch_type<__half, 128>(k, mk, mv, s);
 }
 
 }  // namespace spechub
