@@ -106,7 +106,8 @@ size_t spechub_tree_attention_workspace_bytes(const spechub_cache_desc *desc, in
     CacheArgs c = {};
     c.batch = desc->batch; c.nodes = desc->nodes; c.heads = desc->heads; c.kv_heads = desc->kv_heads; c.head_dim = desc->head_dim;
     c.page_shift = __builtin_ctz(static_cast<unsigned>(desc->page_size)); c.table_width = desc->table_width;
-    return attention_workspace(c, shared_len);
+    size_t bytes = 0;
+    return attention_workspace(c, shared_len, &bytes) ? bytes : 0;
 }
 
 int spechub_tree_attention(const spechub_cache_desc *desc, const spechub_heads *q, const spechub_pages *k_cache,
@@ -129,7 +130,8 @@ int spechub_tree_attention(const spechub_cache_desc *desc, const spechub_heads *
     if (rc == SPECHUB_OK) rc = heads_of(out, desc, desc->heads, true, &a.out);
     if (rc != SPECHUB_OK) return rc;
     if (!mask || (shared_len > 0 && !shared_table)) return SPECHUB_ERR_NULL;
-    const size_t need = attention_workspace(a.c, shared_len);
+    size_t need = 0;
+    if (!attention_workspace(a.c, shared_len, &need)) return SPECHUB_ERR_SHAPE;
     if (workspace_bytes < need) return SPECHUB_ERR_WORKSPACE;
     if (need && !workspace) return SPECHUB_ERR_NULL;
     if (need && !at16(workspace)) return SPECHUB_ERR_ALIGN;

@@ -44,31 +44,38 @@ int page_map(int dtype, const PagesPtr &x, const CacheArgs &c, CUtensorMap *map)
 
 size_t up(size_t n) { return (n + 255) & ~size_t(255); }
 
-// The plan, and the workspace's size; its parts are at `base`.
-size_t plan_of(const CacheArgs &c, int64_t shared_len, uint8_t *base, AttPlan *p) {
-    const int64_t own = static_cast<int64_t>(c.nodes) * (c.heads / c.kv_heads), all = own * c.batch;
+// The plan, and the workspace's size; its parts are at `base`.  false: costs are counted in 31 bits, and there may be more than that.
+bool plan_of(const CacheArgs &c, int64_t shared_len, uint8_t *base, AttPlan *p, size_t *bytes) {
+    const int64_t group = c.heads / c.kv_heads, own = c.nodes * group, all = own * c.batch;
     p->shared_tiles = static_cast<int>((shared_len + kTile - 1) / kTile);
     p->shared_blocks = shared_len ? static_cast<int>((all + kBlockRows - 1) / kBlockRows) : 0;
     p->own_blocks = static_cast<int>((own + kBlockRows - 1) / kBlockRows);
     p->shared_rows = static_cast<int>(all < kBlockRows ? all : kBlockRows);
     p->own_rows = static_cast<int>(own < kBlockRows ? own : kBlockRows);
-    p->shared_items = static_cast<int64_t>(c.kv_heads) * p->shared_blocks;
-    p->shared_units = p->shared_items * p->shared_tiles;
-    // as many CTAs as there can be units, at most one per SM
-    const int64_t own_items = static_cast<int64_t>(c.batch) * c.kv_heads * p->own_blocks;
-    const int64_t most = p->shared_units + own_items * (((static_cast<int64_t>(c.table_width) << c.page_shift) + kTile - 1) / kTile);
-    p->grid = static_cast<int>(most < kSms ? most : kSms);
-    p->slots = shared_len ? p->shared_items + p->grid : 0;
+    const int64_t shared_items = static_cast<int64_t>(c.kv_heads) * p->shared_blocks, own_items = static_cast<int64_t>(c.batch) * c.kv_heads * p->own_blocks;
+    const int64_t own_tiles = ((static_cast<int64_t>(c.table_width) << c.page_shift) + kTile - 1) / kTile;   // of a sequence, at most
+    const int64_t shared_cost = shared_len ? shared_items * (kBlockCost + static_cast<int64_t>(kTileCost) * p->shared_tiles) : 0;
+    const double most = double(shared_cost) + double(own_items) * (kBlockCost + double(kTileCost) * own_tiles);
+    if (most > 2.0e9) return false;
+    p->shared_items = static_cast<int>(shared_items);
+    p->shared_cost = static_cast<int>(shared_cost);
+    p->group = FastDiv::of(static_cast<uint32_t>(group));
+    p->nodes = FastDiv::of(static_cast<uint32_t>(c.nodes));
+    // as many CTAs as there can be tiles, at most one per SM
+    const int64_t tiles = shared_items * p->shared_tiles + own_items * own_tiles;
+    p->grid = static_cast<int>(tiles < kSms ? tiles : kSms);
+    p->slots = shared_len ? shared_items + p->grid : 0;
     const int64_t rows = p->slots * p->shared_rows + (own_items + p->grid) * p->own_rows;
     size_t at = 0;
-    p->before = reinterpret_cast<int64_t *>(base);
-    at += up(sizeof(int64_t) * (static_cast<size_t>(c.batch) + 1));
+    p->before = reinterpret_cast<int *>(base);
+    at += up(sizeof(int) * (static_cast<size_t>(c.batch) + 1));
     p->error = reinterpret_cast<int *>(base + at);
     at += up(sizeof(int) * static_cast<size_t>(p->grid));
     p->ml = reinterpret_cast<float2 *>(base + at);
     at += up(sizeof(float2) * static_cast<size_t>(rows));
     p->o = reinterpret_cast<float *>(base + at);
-    return at + up(sizeof(float) * static_cast<size_t>(rows) * c.head_dim);
+    *bytes = at + up(sizeof(float) * static_cast<size_t>(rows) * c.head_dim);
+    return true;
 }
 
 template <class T, int D>
@@ -78,22 +85,24 @@ int launch_type(const AttKernelArgs &k, const CUtensorMap &mk, const CUtensorMap
     if (rc != SPECHUB_OK) return rc;
     const int lrc = launch_grid(attention_kernel<T, D>, k.p.grid, kAttThreads, AttShape<D>::kSmem, 1, s, k, mk, mv);
     if (lrc != SPECHUB_OK) return lrc;
-    const int64_t rows = static_cast<int64_t>(k.a.c.batch) * k.a.c.nodes * k.a.c.heads, per = kJoinThreads / 32;
-    const unsigned grid = static_cast<unsigned>((rows + per - 1) / per + (k.a.c.status ? k.a.c.batch : 0));
-    return launch_grid(attention_join_kernel<T, D>, grid, kJoinThreads, 0, 1, s, k);
+    const int64_t grid = static_cast<int64_t>(k.a.c.batch) * k.a.c.kv_heads * k.p.own_blocks * ((k.p.own_rows + kJoinRows - 1) / kJoinRows) +
+                         (k.a.c.status ? k.a.c.batch : 0);
+    if (grid > 0x7fffffffLL) return SPECHUB_ERR_SHAPE;
+    return launch_grid(attention_join_kernel<T, D>, static_cast<unsigned>(grid), kJoinThreads, 0, 1, s, k);
 }
 
 }  // namespace
 
-size_t attention_workspace(const CacheArgs &c, int64_t shared_len) {
+bool attention_workspace(const CacheArgs &c, int64_t shared_len, size_t *bytes) {
     AttPlan p;
-    return plan_of(c, shared_len, nullptr, &p);
+    return plan_of(c, shared_len, nullptr, &p, bytes);
 }
 
 int launch_attention(int dtype, const AttentionArgs &a, void *workspace, cudaStream_t s) {
     AttKernelArgs k;
     k.a = a;
-    plan_of(a.c, a.shared_len, static_cast<uint8_t *>(workspace), &k.p);
+    size_t bytes;
+    if (!plan_of(a.c, a.shared_len, static_cast<uint8_t *>(workspace), &k.p, &bytes)) return SPECHUB_ERR_SHAPE;
     CUtensorMap mk, mv;
     int rc = page_map(dtype, a.c.k, a.c, &mk);
     if (rc == SPECHUB_OK) rc = page_map(dtype, a.c.v, a.c, &mv);

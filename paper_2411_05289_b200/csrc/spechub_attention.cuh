@@ -33,9 +33,6 @@ constexpr int kTile = 128;         // keys of a tile, rows of a softmax group
 constexpr int kBlockRows = 256;
 constexpr int kAttThreads = 384;
 constexpr float kSlack = 8.f;
-// Costs of a unit in the split of the work, shared : own.
-constexpr int kCostShared = 1, kCostOwn = 1;
-
 // Weights are stored as 2^bias times themselves.  fp16 has numbers down to 2^-24 only: with the reference 7 below, weights of
 // 2^-31 of the largest still count, and the largest is 2^(7 + kSlack) < 65504.
 template <class T> struct Weight;
@@ -53,12 +50,27 @@ struct AttShape {
     static constexpr int kS = 0, kO = 256, kP = D == 64 ? 384 : 0, kPStep = D == 64 ? 64 : 128;
 };
 
-// What the host knows of the work.
+// x / d for x < 2^31 by a product (Granlund, Montgomery: Division by invariant integers using multiplication).
+struct FastDiv {
+    uint32_t d, m, s;
+    __host__ static FastDiv of(uint32_t d) {
+        uint32_t s = 0;
+        while ((1ull << s) < d) ++s;
+        return FastDiv{d, static_cast<uint32_t>((((1ull << s) - d) << 32) / d + 1), s};
+    }
+    __device__ uint32_t quot(uint32_t x) const { return (__umulhi(m, x) + x) >> s; }
+};
+
+// What the host knows of the work.  A block of `tiles` tiles costs kBlockCost + tiles * (shared_cost or own_cost), and the CTAs share
+// the sum of the costs evenly.
+constexpr int kBlockCost = 6, kTileCost = 4;
 struct AttPlan {
     int shared_tiles, shared_blocks, own_blocks, grid;   // tiles of the prefix; row blocks per cache head: of all rows, of a sequence
     int shared_rows, own_rows;                           // rows of a slot in the workspace
-    int64_t shared_items, shared_units, slots;           // slots of the shared pieces
-    int64_t *before;                                     // [batch + 1] own units before sequence b
+    int shared_items, shared_cost;                       // blocks of the prefix, what they cost
+    int64_t slots;                                       // slots of the shared pieces
+    FastDiv group, nodes;
+    int *before;                                         // [batch + 1] cost of the own blocks before sequence b
     int *error;                                          // [grid]
     float2 *ml;                                          // (reference, sum) of every row of every slot
     float *o;                                            // [..][head_dim], not divided by the sum
@@ -69,102 +81,104 @@ struct AttKernelArgs {
     AttPlan p;
 };
 
-__device__ __forceinline__ int64_t own_end(const CacheArgs &c, int len) {   // keys of a sequence that is there
+__device__ __forceinline__ int own_end(const CacheArgs &c, int len) {   // keys of a sequence that is there
     const int64_t slots = static_cast<int64_t>(c.table_width) << c.page_shift;
-    return min(static_cast<int64_t>(len) + c.nodes, slots);
+    return static_cast<int>(min(static_cast<int64_t>(len) + c.nodes, slots));
 }
 __device__ __forceinline__ int own_tiles(const CacheArgs &c, int len) {
-    return len < 0 ? 0 : static_cast<int>((own_end(c, len) + kTile - 1) / kTile);
+    return len < 0 ? 0 : static_cast<int>((static_cast<unsigned>(own_end(c, len)) + kTile - 1) / kTile);
 }
-// Units are numbered: all of the shared prefix, then sequence by sequence.  CTA i takes those whose cost before them is in
-// [i, i + 1) / grid of the whole.
-struct AttSplit {
-    int64_t shared_units, units, cost;
-    int grid;
-    __device__ AttSplit(const AttPlan &p, int64_t own_units)
-        : shared_units(p.shared_units), units(p.shared_units + own_units), cost(p.shared_units * kCostShared + own_units * kCostOwn), grid(p.grid) {}
-    __device__ int64_t first(int cta) const {
-        const int64_t y = (cta * cost + grid - 1) / grid, s = shared_units * kCostShared;
-        return y <= s ? (y + kCostShared - 1) / kCostShared : shared_units + (y - s + kCostOwn - 1) / kCostOwn;
-    }
-    __device__ int cta(int64_t unit) const {
-        const int64_t before = unit <= shared_units ? unit * kCostShared : shared_units * kCostShared + (unit - shared_units) * kCostOwn;
-        return static_cast<int>(before * grid / cost);
-    }
-};
+__device__ __forceinline__ int block_cost(int tiles) { return tiles ? kBlockCost + tiles * kTileCost : 0; }
+// tiles of a block that lie before `cost`, counted from the block's start
+__device__ __forceinline__ int tiles_before(int cost, int tiles) {
+    return min(tiles, max(0, (cost - kBlockCost + kTileCost - 1) / kTileCost));
+}
+// Blocks are numbered: all of the shared prefix, then sequence by sequence.  Of the whole cost `all`, CTA i takes [first(i), first(i + 1)).
+__device__ __forceinline__ int split_first(int cta, int all, int grid) {
+    const unsigned q = static_cast<unsigned>(all) / grid, r = static_cast<unsigned>(all) - q * grid;
+    return cta * q + (cta * r + grid - 1) / grid;
+}
+__device__ __forceinline__ int split_cta(int cost, int all, int grid) {
+    return static_cast<int>(static_cast<unsigned long long>(static_cast<unsigned>(cost)) * grid / static_cast<unsigned>(all));
+}
 
 // Consecutive tiles of one block of rows.
 struct AttPiece {
     bool shared, two;      // two: more than 128 rows
     int b, head, block, rows, t0, t1, tiles;
-    int64_t item;          // among the shared or among the own blocks
+    int item;              // among the shared or among the own blocks
     int plain, keys;       // keys that every row sees; all keys
-    __device__ bool masked(int t) const { return (t + 1) * int64_t(kTile) > plain; }
+    __device__ bool masked(int t) const { return t >= plain / kTile; }
 };
 
 // The pieces of a CTA's run; every role walks through them by itself.
+struct AttStart { int from, to, at; bool shared; int b, head, block; };   // costs; `at`: where the block begins
 struct AttWalk {
     const CacheArgs &c;
     const AttPlan &p;
-    int shared_len;
-    int64_t left, item;
+    int shared_len, from, to, at, b, head, block, len, tiles;
     bool shared;
-    int b, in_b, tile, len, tiles;
 
-    __device__ AttWalk(const AttKernelArgs &K, int64_t units, bool in_shared, int64_t shared_item, int b0, int in_b0, int tile0)
-        : c(K.a.c), p(K.p), shared_len(K.a.shared_len), left(units), item(shared_item), shared(in_shared), b(b0), in_b(in_b0), tile(tile0), len(0), tiles(0) {
-        if (!shared && left > 0) look();
+    __device__ AttWalk(const AttKernelArgs &K, const AttStart &s)
+        : c(K.a.c), p(K.p), shared_len(K.a.shared_len), from(s.from), to(s.to), at(s.at), b(s.b), head(s.head), block(s.block), shared(s.shared) {
+        look();
     }
     __device__ void look() {
-        len = b < c.batch ? c.lens[b] : -1;
-        tiles = own_tiles(c, len);
+        if (shared) { tiles = p.shared_tiles; return; }
+        tiles = 0;
+        if (at >= to) return;
+        for (; b < c.batch; ++b) {
+            len = c.lens[b];
+            tiles = own_tiles(c, len);
+            if (tiles) break;
+        }
     }
     __device__ bool next(AttPiece &x) {
-        if (left <= 0) return false;
-        x.shared = shared;
-        x.t0 = tile;
-        if (shared) {
-            x.b = 0;
-            x.head = static_cast<int>(item / p.shared_blocks);
-            x.block = static_cast<int>(item % p.shared_blocks);
-            x.item = item;
-            x.tiles = p.shared_tiles;
-            x.plain = x.keys = shared_len;
-            x.rows = min(kBlockRows, c.batch * c.nodes * (c.heads / c.kv_heads) - x.block * kBlockRows);
-        } else {
-            const int per_b = c.kv_heads * p.own_blocks;
-            while (b < c.batch && (in_b == per_b || tiles == 0)) { ++b; in_b = 0; look(); }
-            if (b >= c.batch) return false;
-            x.b = b;
-            x.head = in_b / p.own_blocks;
-            x.block = in_b % p.own_blocks;
-            x.item = static_cast<int64_t>(b) * per_b + in_b;
+        while (at < to && tiles) {
+            x.shared = shared;
+            x.head = head;
+            x.block = block;
             x.tiles = tiles;
-            x.keys = static_cast<int>(own_end(c, len));
-            x.plain = min(len, x.keys);
-            x.rows = min(kBlockRows, c.nodes * (c.heads / c.kv_heads) - x.block * kBlockRows);
-        }
-        x.two = x.rows > kTile;
-        x.t1 = static_cast<int>(min(static_cast<int64_t>(x.tiles), tile + left));
-        left -= x.t1 - x.t0;
-        tile = x.t1;
-        if (tile == x.tiles) {
-            tile = 0;
+            x.t0 = from > at ? tiles_before(from - at, tiles) : 0;
+            x.t1 = tiles_before(to - at, tiles);
+            int rows;
             if (shared) {
-                if (++item == p.shared_items) { shared = false; b = 0; in_b = 0; if (left > 0) look(); }
-            } else ++in_b;
+                x.b = 0;
+                x.item = head * p.shared_blocks + block;
+                x.plain = x.keys = shared_len;
+                rows = c.batch * c.nodes * p.group.d;
+            } else {
+                x.b = b;
+                x.item = (b * c.kv_heads + head) * p.own_blocks + block;
+                x.keys = own_end(c, len);
+                x.plain = min(len, x.keys);
+                rows = c.nodes * p.group.d;
+            }
+            x.rows = min(kBlockRows, rows - block * kBlockRows);
+            x.two = x.rows > kTile;
+            at += block_cost(tiles);
+            if (++block == (shared ? p.shared_blocks : p.own_blocks)) {
+                block = 0;
+                if (++head == c.kv_heads) {
+                    head = 0;
+                    if (shared) { shared = false; b = 0; }
+                    else ++b;
+                    look();
+                }
+            }
+            if (x.t1 > x.t0) return true;
         }
-        return true;
+        return false;
     }
 };
 
 // Where row `i` of a block is.
 struct AttRow { int b, n, h; };
-__device__ __forceinline__ AttRow row_of(const CacheArgs &c, const AttPiece &x, int i) {
-    const unsigned g = c.heads / c.kv_heads, r = x.block * kBlockRows + i, node = r / g;
+__device__ __forceinline__ AttRow row_of(const AttPlan &p, const AttPiece &x, int i) {
+    const unsigned r = x.block * kBlockRows + i, node = p.group.quot(r);
     AttRow o;
-    o.h = x.head * g + (r - node * g);
-    if (x.shared) { o.b = node / c.nodes; o.n = node - o.b * c.nodes; }
+    o.h = x.head * p.group.d + (r - node * p.group.d);
+    if (x.shared) { o.b = p.nodes.quot(node); o.n = node - o.b * p.nodes.d; }
     else { o.b = x.b; o.n = node; }
     return o;
 }
@@ -217,12 +231,12 @@ __global__ void __launch_bounds__(kAttThreads, 1) attention_kernel(const __grid_
     using L = AttShape<D>;
     constexpr bool kBf16 = Weight<T>::kBf16;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ __align__(8) uint64_t bars[2 * L::kStages + 7];
+    __shared__ __align__(8) uint64_t bars[2 * L::kStages + 11];
     __shared__ uint32_t tmem_base;
     __shared__ int gave_up_, bad_values;
     __shared__ float2 other[kTile];           // (reference, sum) of the second group's rows
-    __shared__ int64_t warp_sum[kAttThreads / 32];
-    __shared__ struct { int64_t units, item; int shared, b, in_b, tile; } start;
+    __shared__ int warp_sum[kAttThreads / 32];
+    __shared__ AttStart start;
     volatile int *const gave_up = &gave_up_;
 
     const AttentionArgs &A = K.a;
@@ -233,16 +247,22 @@ __global__ void __launch_bounds__(kAttThreads, 1) attention_kernel(const __grid_
     const uint32_t s_q = saddr(smem), s_kv = s_q + 2 * L::kTileBytes, bar0 = saddr(bars);
     const auto kv_full = [&](int s) { return bar0 + 8u * s; };
     const auto kv_empty = [&](int s) { return bar0 + 8u * (L::kStages + s); };
-    const uint32_t q_full = bar0 + 16u * L::kStages;
-    const auto s_full = [&](int t) { return q_full + 8u + 8u * t; };
-    const auto p_full = [&](int t) { return q_full + 24u + 8u * t; };
-    const auto o_full = [&](int t) { return q_full + 40u + 8u * t; };
+    const uint32_t bar1 = bar0 + 16u * L::kStages;
+    const auto q_full = [&](int q) { return bar1 + 8u * q; };
+    const auto q_empty = [&](int q) { return bar1 + 16u + 8u * q; };
+    const auto s_full = [&](int t) { return bar1 + 32u + 8u * t; };
+    const auto p_full = [&](int t) { return bar1 + 48u + 8u * t; };
+    const auto o_full = [&](int t) { return bar1 + 64u + 8u * t; };
+    const uint32_t o_free = bar1 + 80u;
 
     if (warp == 9) tmem_alloc(saddr(&tmem_base), 512);
     if (tid == 0) {
         for (int s = 0; s < L::kStages; ++s) { bar_init(kv_full(s), 1); bar_init(kv_empty(s), 1); }
-        bar_init(q_full, 256);
-        for (int t = 0; t < 2; ++t) { bar_init(s_full(t), 1); bar_init(p_full(t), kTile); bar_init(o_full(t), 1); }
+        for (int t = 0; t < 2; ++t) {
+            bar_init(q_full(t), 64); bar_init(q_empty(t), 1);
+            bar_init(s_full(t), 1); bar_init(p_full(t), kTile); bar_init(o_full(t), 1);
+        }
+        bar_init(o_free, 2 * kTile);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         gave_up_ = 0;
         bad_values = 0;
@@ -251,56 +271,64 @@ __global__ void __launch_bounds__(kAttThreads, 1) attention_kernel(const __grid_
     }
     pdl_begin();
 
-    // This CTA's run of units: own units of all sequences summed up, in the order of the sequences.
+    // This CTA's run: own costs of all sequences summed up, in the order of the sequences.
     {
         const int per = (c.batch + kAttThreads - 1) / kAttThreads, b0 = min(c.batch, tid * per), b1 = min(c.batch, b0 + per);
-        const int64_t per_b = static_cast<int64_t>(c.kv_heads) * P.own_blocks;
-        int64_t mine = 0;
-        for (int b = b0; b < b1; ++b) mine += own_tiles(c, c.lens[b]) * per_b;
-        int64_t upto = mine;
+        const int per_b = c.kv_heads * P.own_blocks;
+        int last = 0, mine = 0;   // of the thread's only or last sequence
+        for (int b = b0; b < b1; ++b) {
+            last = block_cost(own_tiles(c, c.lens[b]));
+            mine += last * per_b;
+        }
+        int upto = mine;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const int64_t v = __shfl_up_sync(kFull, upto, o);
+            const int v = __shfl_up_sync(kFull, upto, o);
             if (lane >= o) upto += v;
         }
         if (lane == 31) warp_sum[warp] = upto;
         __syncthreads();
-        int64_t all = 0;
+        int all = P.shared_cost;
+#pragma unroll
         for (int w = 0; w < kAttThreads / 32; ++w) {
-            if (w < warp) upto += warp_sum[w];
-            all += warp_sum[w];
+            const int v = warp_sum[w];
+            if (w < warp) upto += v;
+            all += v;
         }
-        const AttSplit split(P, all);
-        const int64_t u0 = split.first(blockIdx.x), u1 = min(split.units, split.first(blockIdx.x + 1));
-        int64_t before = upto - mine;
-        if (tid == 0) {
-            start.units = max(int64_t(0), u1 - u0);
-            start.shared = u0 < P.shared_units;
-            start.item = start.shared ? u0 / P.shared_tiles : 0;
-            start.tile = start.shared ? static_cast<int>(u0 % P.shared_tiles) : 0;
-            start.b = 0; start.in_b = 0;
+        upto += P.shared_cost;
+        const int from = split_first(blockIdx.x, all, P.grid), to = split_first(blockIdx.x + 1, all, P.grid);
+        int before = upto - mine;
+        const bool here = from >= before && from < upto;
+        if (tid == 0 && from == to) start = AttStart{0, 0, 0, false, 0, 0, 0};
+        if (tid == 0 && from < to && from < P.shared_cost) {
+            const int each = block_cost(P.shared_tiles), item = from / each;
+            start = AttStart{from, to, item * each, true, 0, item / P.shared_blocks, item % P.shared_blocks};
         }
-        __syncthreads();
-        const int64_t uo = u0 - P.shared_units;
-        const bool here = uo >= before && uo < upto;
-        if (here || (blockIdx.x == 0 && b0 < b1)) {
-            for (int b = b0; b < b1; ++b) {
-                const int64_t n = own_tiles(c, c.lens[b]) * per_b;
-                if (here && uo >= before && uo < before + n) {
-                    const int64_t in = uo - before, tiles = n / per_b;
-                    start.b = b; start.in_b = static_cast<int>(in / tiles); start.tile = static_cast<int>(in % tiles);
+        if (here && from < to) {
+            int b = b0;
+            if (per > 1)
+                for (; b < b1; ++b) {
+                    last = block_cost(own_tiles(c, c.lens[b]));
+                    if (from < before + last * per_b) break;
+                    before += last * per_b;
                 }
-                if (blockIdx.x == 0) P.before[b] = before;
-                before += n;
+            const int in_b = (from - before) / last;
+            start = AttStart{from, to, before + in_b * last, false, b, in_b / P.own_blocks, in_b % P.own_blocks};
+        }
+        if (blockIdx.x == 0 && b0 < b1) {   // for the kernel that joins
+            before = upto - mine;
+            for (int b = b0; b < b1; ++b) {
+                P.before[b] = before;
+                before += block_cost(own_tiles(c, c.lens[b])) * per_b;
             }
-            if (blockIdx.x == 0 && b1 == c.batch) P.before[c.batch] = before;
+            if (b1 == c.batch) P.before[c.batch] = before;
         }
         tmem_fence_before();
         __syncthreads();
         tmem_fence_after();
     }
     const uint32_t tm = tmem_base;
-    AttWalk walk(K, start.units, start.shared, start.item, start.b, start.in_b, start.tile);
+    AttWalk walk(K, start);
     AttPiece x = {};
 
     if (warp == 8) {
@@ -352,7 +380,8 @@ __global__ void __launch_bounds__(kAttThreads, 1) attention_kernel(const __grid_
     } else if (warp == 9) {
         // ---- matrix instructions -------------------------------------------------------------------
         int stage = 0;
-        uint32_t phase = 0, q_phase = 0, p_phase[2] = {0, 0};
+        uint32_t phase = 0, q_phase = 0, p_phase[2] = {0, 0}, free_phase = 1;
+        int q_slot = 0;
         constexpr uint32_t desc_s = mma_desc(kBf16, kTile, false), desc_o = mma_desc(kBf16, D, true);
         const auto arrived = [&]() {   // the next stage of the ring
             bar_wait(kv_full(stage), phase, gave_up);
@@ -383,42 +412,67 @@ __global__ void __launch_bounds__(kAttThreads, 1) attention_kernel(const __grid_
         // values behind the end, and those of tree nodes that are no numbers: zero
         const auto clear = [&](int tile, int s) {
             constexpr int kVecs = D / 8;
+            constexpr uint32_t kExp = kBf16 ? 0x7f807f80u : 0x7c007c00u;   // all ones: no finite number
             const int r0 = max(0, x.plain - tile * kTile), r1 = min(kTile, x.keys - tile * kTile);
             uint8_t *const v = smem + 2 * L::kTileBytes + s * L::kTileBytes;
+            const auto at = [&](int i) { return reinterpret_cast<uint4 *>(v + (i % kVecs / 8) * L::kHalfBytes + (i / kVecs) * 128 + (i % 8) * 16); };
             bool bad = false;
-            for (int i = lane + r0 * kVecs; i < kTile * kVecs; i += 32) {
-                const int r = i / kVecs, h = i % kVecs / 8, vec = i % 8;
-                uint4 *at = reinterpret_cast<uint4 *>(v + h * L::kHalfBytes + r * 128 + vec * 16);
-                if (r >= r1) { *at = make_uint4(0, 0, 0, 0); continue; }
-                uint4 u = *at;
-                uint32_t *w = &u.x;
-                bool any = false;
+            for (int i = lane + r0 * kVecs; i < r1 * kVecs; i += 128) {
+                uint4 u[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) u[j] = i + 32 * j < r1 * kVecs ? *at(i + 32 * j) : make_uint4(0, 0, 0, 0);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    if (not_finite<T>(w[j] & 0xffff)) { w[j] &= 0xffff0000u; any = true; }
-                    if (not_finite<T>(w[j] >> 16)) { w[j] &= 0xffffu; any = true; }
+                    uint32_t *w = &u[j].x, hit = 0;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const uint32_t t = (w[k] & kExp) ^ kExp;   // a half that is zero: no finite number
+                        hit |= (t - 0x00010001u) & ~t & 0x80008000u;
+                    }
+                    if (hit) {
+                        bad = true;
+                        for (int k = 0; k < 4; ++k) {
+                            if ((w[k] & kExp & 0xffffu) == (kExp & 0xffffu)) w[k] &= 0xffff0000u;
+                            if ((w[k] & kExp & 0xffff0000u) == (kExp & 0xffff0000u)) w[k] &= 0xffffu;
+                        }
+                        *at(i + 32 * j) = u[j];
+                    }
                 }
-                if (any) *at = u;
-                bad |= any;
             }
+            for (int i = lane + r1 * kVecs; i < kTile * kVecs; i += 32) *at(i) = make_uint4(0, 0, 0, 0);
             if (__any_sync(kFull, bad) && lane == 0) *static_cast<volatile int *>(&bad_values) = 1;
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __threadfence_block();
             __syncwarp();
         };
         while (walk.next(x)) {
-            bar_wait(q_full, q_phase, gave_up);
-            q_phase ^= 1u;
+            // queries of both groups, or of one block in whichever slot is next
+            int q[2];
+            for (int i = 0; i < (x.two ? 2 : 1); ++i) {
+                q[i] = q_slot;
+                bar_wait(q_full(q_slot), q_phase, gave_up);
+                if (++q_slot == 2) { q_slot = 0; q_phase ^= 1u; }
+            }
+            const int ahead = x.two ? 1 : 2;
+            const auto last_scores = [&](int t) {   // after those of tile t: is a slot of queries free?
+                if (t == x.t1 - 1 && lane == 0) {
+                    mma_commit(q_empty(q[0]));
+                    if (x.two) mma_commit(q_empty(q[1]));
+                }
+            };
+            for (int i = 0; i < ahead && x.t0 + i < x.t1; ++i) {
+                const int s = arrived();
+                scores(i, q[0], s);
+                if (x.two) scores(1, q[1], s);
+                if (lane == 0) mma_commit(kv_empty(s));
+                last_scores(x.t0 + i);
+            }
+            // O of the piece before has been read by now or soon, and what was said of its values
+            bar_wait(o_free, free_phase, gave_up);
+            free_phase ^= 1u;
             tmem_fence_after();
             if (lane == 0) *static_cast<volatile int *>(&bad_values) = 0;
             __syncwarp();
-            const int ahead = x.two ? 1 : 2;
-            for (int i = 0; i < ahead && x.t0 + i < x.t1; ++i) {
-                const int s = arrived();
-                scores(i, 0, s);
-                if (x.two) scores(1, 1, s);
-                if (lane == 0) mma_commit(kv_empty(s));
-            }
             for (int t = x.t0; t < x.t1; ++t) {
                 const int v = arrived();
                 if (x.masked(t)) clear(t, v);
@@ -427,7 +481,7 @@ __global__ void __launch_bounds__(kAttThreads, 1) attention_kernel(const __grid_
                     const int s = more ? arrived() : 0;
                     for (int g = 0; g < 2; ++g) {
                         products(g, v, t > x.t0);
-                        if (more) scores(g, g, s);
+                        if (more) scores(g, q[g], s);
                         else if (lane == 0) mma_commit(o_full(g));
                     }
                     if (lane == 0) {
@@ -440,11 +494,47 @@ __global__ void __launch_bounds__(kAttThreads, 1) attention_kernel(const __grid_
                     if (lane == 0) mma_commit(kv_empty(v));
                     if (more) {
                         const int s = arrived();
-                        scores(g, 0, s);
+                        scores(g, q[0], s);
                         if (lane == 0) mma_commit(kv_empty(s));
                     } else if (lane == 0) mma_commit(o_full(g));
                 }
+                if (more) last_scores(t + ahead);
             }
+        }
+        // (the last arrivals come before the CTA ends)
+        bar_wait(o_free, free_phase, gave_up);
+    } else if (warp >= 10) {
+        // ---- queries -----------------------------------------------------------------------------------
+        constexpr int kVecs = D / 8, kStep = 64 / kVecs, kBatch = 16;   // rows that the two warps bring at once; loads in flight per thread
+        int slot = 0;
+        uint32_t phase = 1;
+        const int qt = tid - 320, vec = qt % kVecs;
+        while (walk.next(x)) {
+            for (int i = 0; i < (x.two ? 2 : 1); ++i) {
+                bar_wait(q_empty(slot), phase, gave_up);
+                uint8_t *dst = smem + slot * L::kTileBytes + (vec / 8) * L::kHalfBytes;
+                const int rows = min(kTile, x.rows - i * kTile);   // (what the other rows hold matters to nobody)
+                for (int r0 = qt / kVecs; r0 < rows; r0 += kBatch * kStep) {
+                    uint4 u[kBatch];
+#pragma unroll
+                    for (int j = 0; j < kBatch; ++j) {
+                        const AttRow o = row_of(P, x, i * kTile + min(rows - 1, r0 + j * kStep));
+                        u[j] = *reinterpret_cast<const uint4 *>(static_cast<const T *>(A.q.data) + o.b * A.q.seq + o.n * A.q.node + o.h * A.q.head + vec * 8);
+                    }
+#pragma unroll
+                    for (int j = 0; j < kBatch; ++j) {
+                        const int r = r0 + j * kStep;
+                        if (r < rows) *reinterpret_cast<uint4 *>(dst + r * 128 + ((vec & 7) ^ (r & 7)) * 16) = u[j];
+                    }
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                bar_arrive(q_full(slot));
+                if (++slot == 2) { slot = 0; phase ^= 1u; }
+            }
+        }
+        for (int i = 0; i < 2; ++i) {
+            bar_wait(q_empty(slot), phase, gave_up);
+            if (++slot == 2) { slot = 0; phase ^= 1u; }
         }
     } else if (warp < 8) {
         // ---- softmax ---------------------------------------------------------------------------------
@@ -454,27 +544,9 @@ __global__ void __launch_bounds__(kAttThreads, 1) attention_kernel(const __grid_
         uint32_t s_phase = 0, o_phase = 0;
         const float cs = A.scale_log2;
         while (walk.next(x)) {
-            {   // queries: of this group's rows, or half of the rows that both have
-                constexpr int kVecs = D / 8, kStep = kTile / kVecs;
-                const int q = x.two ? g : 0, r0 = x.two ? 0 : g * (kTile / 2), r1 = x.two ? kTile : r0 + kTile / 2;
-                const int vec = gt % kVecs;
-                uint8_t *dst = smem + q * L::kTileBytes + (vec / 8) * L::kHalfBytes;
-#pragma unroll 4
-                for (int r = r0 + gt / kVecs; r < r1; r += kStep) {
-                    uint4 u = make_uint4(0, 0, 0, 0);
-                    if (q * kTile + r < x.rows) {
-                        const AttRow o = row_of(c, x, q * kTile + r);
-                        u = *reinterpret_cast<const uint4 *>(static_cast<const T *>(A.q.data) + o.b * A.q.seq + o.n * A.q.node + o.h * A.q.head + vec * 8);
-                    }
-                    *reinterpret_cast<uint4 *>(dst + r * 128 + ((vec & 7) ^ (r & 7)) * 16) = u;
-                }
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                tmem_fence_before();
-                bar_arrive(q_full);
-            }
             const int row = (x.two ? g * kTile : 0) + gt;
             const bool warp_on = row - lane < x.rows;   // any row in this warp
-            const AttRow at = row_of(c, x, min(row, x.rows - 1));
+            const AttRow at = row_of(P, x, min(row, x.rows - 1));
             float ref = neg_inf(), sum = 0.f;
             const int step = x.two ? 1 : 2, first = x.two ? x.t0 : x.t0 + g;
             for (int t = first; t < x.t1; t += step) {
@@ -482,29 +554,35 @@ __global__ void __launch_bounds__(kAttThreads, 1) attention_kernel(const __grid_
                 s_phase ^= 1u;
                 tmem_fence_after();
                 if (warp_on) {
-                    float s[kTile];
+                    // twice through the scores, 32 at a time (a row of 128 would not fit the registers): maximum, weights
+                    const bool masked = x.masked(t);
+                    uint32_t bits[4] = {~0u, ~0u, ~0u, ~0u};
+                    if (masked) row_bits(A, x, t, at.n, bits);
+                    float s[2][32], m0 = neg_inf(), m1 = neg_inf(), m2 = neg_inf(), m3 = neg_inf();
+                    const auto hide = [&](float *y, uint32_t b) {
+                        if (masked) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) tmem_ld32_async(t_s + 32 * i, s + 32 * i);
-                    tmem_wait_ld();
+                            for (int i = 0; i < 32; ++i) y[i] = b >> i & 1 ? y[i] : neg_inf();
+                        }
+                    };
+                    tmem_ld32_async(t_s, s[0]);
 #pragma unroll
-                    for (int i = 0; i < kTile; ++i) asm volatile("" : "+f"(s[i]));
-                    if (x.masked(t)) {
-                        uint32_t bits[4];
-                        row_bits(A, x, t, at.n, bits);
+                    for (int h = 0; h < 4; ++h) {
+                        float *y = s[h & 1];
+                        tmem_wait_ld32(y);
+                        if (h < 3) tmem_ld32_async(t_s + 32 * (h + 1), s[~h & 1]);
+                        hide(y, bits[h]);
 #pragma unroll
-                        for (int i = 0; i < kTile; ++i) s[i] = bits[i / 32] >> (i & 31) & 1 ? s[i] : neg_inf();
-                    }
-                    float m0 = neg_inf(), m1 = neg_inf(), m2 = neg_inf(), m3 = neg_inf();
-#pragma unroll
-                    for (int i = 0; i < kTile; i += 8) {
-                        m0 = fmaxf(m0, fmaxf(s[i], s[i + 1]));
-                        m1 = fmaxf(m1, fmaxf(s[i + 2], s[i + 3]));
-                        m2 = fmaxf(m2, fmaxf(s[i + 4], s[i + 5]));
-                        m3 = fmaxf(m3, fmaxf(s[i + 6], s[i + 7]));
+                        for (int i = 0; i < 32; i += 8) {
+                            m0 = fmaxf(m0, fmaxf(y[i], y[i + 1]));
+                            m1 = fmaxf(m1, fmaxf(y[i + 2], y[i + 3]));
+                            m2 = fmaxf(m2, fmaxf(y[i + 4], y[i + 5]));
+                            m3 = fmaxf(m3, fmaxf(y[i + 6], y[i + 7]));
+                        }
                     }
                     const float top = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3)) * cs - Weight<T>::kBias;
                     if (t == first) ref = top;
-                    else if (__any_sync(kFull, top > ref + kSlack)) {
+                    else if (__any_sync(kFull, top > ref + kSlack && row < x.rows)) {
                         // (the product that added the last tile to O is done: it was issued before these scores)
                         const float now = fmaxf(ref, top), f = now == neg_inf() ? 1.f : ex2(ref - now);
                         sum *= f;
@@ -518,21 +596,25 @@ __global__ void __launch_bounds__(kAttThreads, 1) attention_kernel(const __grid_
                             tmem_st32(t_o + g * D + i, o);
                         }
                     }
+                    tmem_ld32_async(t_s, s[0]);
                     const float sub = ref == neg_inf() ? 0.f : -ref;
                     float l0 = 0.f, l1 = 0.f, l2 = 0.f, l3 = 0.f;
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        uint32_t w[32];
+                    for (int h = 0; h < 4; ++h) {
+                        float *y = s[h & 1];
+                        uint32_t w[16];
+                        tmem_wait_ld32(y);
+                        if (h < 3) tmem_ld32_async(t_s + 32 * (h + 1), s[~h & 1]);
+                        hide(y, bits[h]);
 #pragma unroll
-                        for (int i = 0; i < 32; i += 2) {
-                            const float *y = s + 64 * h + 2 * i;
-                            const float a = ex2(fmaf(y[0], cs, sub)), b = ex2(fmaf(y[1], cs, sub));
-                            const float e = ex2(fmaf(y[2], cs, sub)), f = ex2(fmaf(y[3], cs, sub));
+                        for (int i = 0; i < 32; i += 4) {
+                            const float a = ex2(fmaf(y[i], cs, sub)), b = ex2(fmaf(y[i + 1], cs, sub));
+                            const float e = ex2(fmaf(y[i + 2], cs, sub)), f = ex2(fmaf(y[i + 3], cs, sub));
                             l0 += a; l1 += b; l2 += e; l3 += f;
-                            w[i] = pack2<T>(a, b);
-                            w[i + 1] = pack2<T>(e, f);
+                            w[i / 2] = pack2<T>(a, b);
+                            w[i / 2 + 1] = pack2<T>(e, f);
                         }
-                        tmem_st32_async(t_p + 32 * h, w);
+                        tmem_st16_async(t_p + 16 * h, w);   // (over scores that all have been read)
                     }
                     sum += (l0 + l1) + (l2 + l3);
                     tmem_wait_st();
@@ -570,8 +652,8 @@ __global__ void __launch_bounds__(kAttThreads, 1) attention_kernel(const __grid_
                 const int bad = *static_cast<volatile int *>(&bad_values);
                 int64_t slot_row = 0;
                 if (!whole) {
-                    slot_row = x.shared ? (x.item + blockIdx.x) * P.shared_rows + row
-                                        : P.slots * P.shared_rows + (x.item + blockIdx.x) * P.own_rows + row;
+                    slot_row = x.shared ? (x.item + int64_t(blockIdx.x)) * P.shared_rows + row
+                                        : P.slots * P.shared_rows + (x.item + int64_t(blockIdx.x)) * P.own_rows + row;
                     if (mine) P.ml[slot_row] = make_float2(ref, sum);
                 } else if (mine && A.lse) {
                     A.lse[(static_cast<int64_t>(at.b) * c.nodes + at.n) * c.heads + at.h] = none ? neg_inf() : (ref + log2f(sum)) * 0.6931471805599453f;
@@ -611,22 +693,25 @@ __global__ void __launch_bounds__(kAttThreads, 1) attention_kernel(const __grid_
                     __syncwarp();
                 }
             }
+            tmem_fence_before();
+            bar_arrive(o_free);
         }
     }
     tmem_fence_before();
     __syncthreads();
     if (*gave_up) {   // copies that were not waited for are in shared memory long before this ends
-        const unsigned long long t0 = now_ns();
-        while (now_ns() - t0 < 2000000ull) __nanosleep(10000);
+        const long long t0 = clock64();
+        while (clock64() - t0 < 4000000) __nanosleep(10000);
         __syncthreads();
     }
     if (tid == 0) P.error[blockIdx.x] = gave_up_;
     if (warp == 9) tmem_dealloc(tm, 512);
 }
 
-constexpr int kJoinThreads = 256;
+constexpr int kJoinThreads = 256, kJoinRows = 32;
 
-// Joins the pieces of every row that has more than one (a warp per row), and finds bad pages (the first `batch` CTAs, if wanted).
+// Joins the pieces of every block that has more than one, kJoinRows of its rows per CTA, a warp per row; and finds bad pages (the first
+// `batch` CTAs, if wanted).
 template <class T, int D>
 __global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(const __grid_constant__ AttKernelArgs K) {
     constexpr int E = D / 32;
@@ -635,9 +720,9 @@ __global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(const __gr
     const CacheArgs &c = A.c;
     const AttPlan &P = K.p;
     const int tid = threadIdx.x, lane = tid & 31;
-    unsigned block = blockIdx.x;
+    int block = blockIdx.x;
     if (c.status) {
-        if (block < static_cast<unsigned>(c.batch)) {
+        if (block < c.batch) {
             const int b = block, ps = 1 << c.page_shift, len = c.lens[b];
             bool bad = false, error = false;
             if (len >= 0) {
@@ -656,47 +741,49 @@ __global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(const __gr
         }
         block -= c.batch;
     }
-    const int64_t at = block * int64_t(kJoinThreads / 32) + (tid >> 5);
-    if (at >= static_cast<int64_t>(c.batch) * c.nodes * c.heads) return;
-    const int h = at % c.heads, n = at / c.heads % c.nodes, b = static_cast<int>(at / c.heads / c.nodes);
+    const int chunks = (P.own_rows + kJoinRows - 1) / kJoinRows, chunk = block % chunks;
+    const int item = block / chunks, per_b = c.kv_heads * P.own_blocks, b = item / per_b, in_b = item - b * per_b;
     const int len = c.lens[b];
     if (len < 0) return;
-    const int g = c.heads / c.kv_heads, hk = h / g, own_row = n * g + (h - hk * g), tiles = own_tiles(c, len);
-    const AttSplit split(P, P.before[c.batch]);
-    const int in_b = hk * P.own_blocks + own_row / kBlockRows;
-    const int64_t own_item = static_cast<int64_t>(b) * c.kv_heads * P.own_blocks + in_b;
-    const int64_t own0 = P.shared_units + P.before[b] + static_cast<int64_t>(in_b) * tiles, own1 = own0 + tiles;
-    if (P.shared_tiles == 0 && split.cta(own0) == split.cta(own1 - 1)) return;   // finished in place
-    const int64_t all_row = static_cast<int64_t>(b) * c.nodes * g + own_row, shared_item = P.shared_tiles ? hk * static_cast<int64_t>(P.shared_blocks) + all_row / kBlockRows : 0;
-    float ref = neg_inf(), sum = 0.f, o[E] = {};
-    const auto add = [&](int64_t slot_row) {
-        const float2 ml = P.ml[slot_row];
-        float z[E];
-        const float *src = P.o + slot_row * D + lane * E;
-        if (E == 4) { const float4 v = *reinterpret_cast<const float4 *>(src); z[0] = v.x; z[1] = v.y; z[E - 2] = v.z; z[E - 1] = v.w; }
-        else { const float2 v = *reinterpret_cast<const float2 *>(src); z[0] = v.x; z[1] = v.y; }
-        const float now = fmaxf(ref, ml.x), r = now == neg_inf() ? 0.f : now, f0 = ex2(ref - r), f1 = ex2(ml.x - r);
-        sum = sum * f0 + ml.y * f1;
-        ref = now;
+    const int tiles = own_tiles(c, len), each = block_cost(tiles), all = P.before[c.batch];
+    const int own0 = P.before[b] + in_b * each;                       // the block's cost interval, and where its tiles begin
+    const int c0 = split_cta(own0 + kBlockCost, all, P.grid), c1 = split_cta(own0 + each - 1, all, P.grid);
+    if (P.shared_tiles == 0 && tiles_before(split_first(c0 + 1, all, P.grid) - own0, tiles) == tiles) return;   // finished in place
+    const int hk = in_b / P.own_blocks, first = (in_b - hk * P.own_blocks) * kBlockRows, rows = min(P.own_rows, c.nodes * static_cast<int>(P.group.d) - first);
+    for (int row = chunk * kJoinRows + (tid >> 5); row < min(rows, (chunk + 1) * kJoinRows); row += kJoinThreads / 32) {
+        float ref = neg_inf(), sum = 0.f, o[E] = {};
+        // pieces of CTAs i0..i1 of a block at `at` in the costs (one whose run has no tile of it left nothing)
+        const auto add = [&](int at, int n, int i0, int i1, int64_t slot_row, int step) {
+            for (int i = i0; i <= i1; ++i) {
+                const int t0 = tiles_before(split_first(i, all, P.grid) - at, n), t1 = tiles_before(split_first(i + 1, all, P.grid) - at, n);
+                if (t1 <= t0) continue;
+                const float2 ml = P.ml[slot_row + int64_t(i) * step];
+                const float *src = P.o + (slot_row + int64_t(i) * step) * D + lane * E;
+                float z[E];
+                if (E == 4) { const float4 v = *reinterpret_cast<const float4 *>(src); z[0] = v.x; z[1] = v.y; z[E - 2] = v.z; z[E - 1] = v.w; }
+                else { const float2 v = *reinterpret_cast<const float2 *>(src); z[0] = v.x; z[1] = v.y; }
+                const float now = fmaxf(ref, ml.x), r = now == neg_inf() ? 0.f : now, f0 = ex2(ref - r), f1 = ex2(ml.x - r);
+                sum = sum * f0 + ml.y * f1;
+                ref = now;
 #pragma unroll
-        for (int i = 0; i < E; ++i) o[i] = o[i] * f0 + z[i] * f1;
-    };
-    for (int64_t u = shared_item * P.shared_tiles, u1 = u + P.shared_tiles; u < u1;) {
-        const int cta = split.cta(u);
-        add((shared_item + cta) * P.shared_rows + all_row % kBlockRows);
-        u = split.first(cta + 1);
-    }
-    for (int64_t u = own0; u < own1;) {
-        const int cta = split.cta(u);
-        add(P.slots * P.shared_rows + (own_item + cta) * P.own_rows + own_row % kBlockRows);
-        u = split.first(cta + 1);
-    }
-    const bool none = sum == 0.f;
-    const float inv = none ? 0.f : 1.f / sum;
-    T *dst = static_cast<T *>(A.out.data) + b * A.out.seq + n * A.out.node + h * A.out.head + lane * E;
+                for (int k = 0; k < E; ++k) o[k] = o[k] * f0 + z[k] * f1;
+            }
+        };
+        if (P.shared_tiles) {
+            const int64_t r = static_cast<int64_t>(b) * c.nodes * P.group.d + first + row;
+            const int in = hk * P.shared_blocks + static_cast<int>(r / kBlockRows), s_each = block_cost(P.shared_tiles), at = in * s_each;
+            add(at, P.shared_tiles, split_cta(at + kBlockCost, all, P.grid), split_cta(at + s_each - 1, all, P.grid),
+                int64_t(in) * P.shared_rows + r % kBlockRows, P.shared_rows);
+        }
+        add(own0, tiles, c0, c1, P.slots * P.shared_rows + int64_t(item) * P.own_rows + row, P.own_rows);
+        const bool none = sum == 0.f;
+        const float inv = none ? 0.f : 1.f / sum;
+        const int n = P.group.quot(first + row), h = hk * P.group.d + (first + row - n * P.group.d);
+        T *dst = static_cast<T *>(A.out.data) + b * A.out.seq + n * A.out.node + h * A.out.head + lane * E;
 #pragma unroll
-    for (int i = 0; i < E; i += 2) *reinterpret_cast<uint32_t *>(dst + i) = pack2<T>(o[i] * inv, o[i + 1] * inv);
-    if (A.lse && lane == 0) A.lse[at] = none ? neg_inf() : (ref + log2f(sum)) * 0.6931471805599453f;
+        for (int i = 0; i < E; i += 2) *reinterpret_cast<uint32_t *>(dst + i) = pack2<T>(o[i] * inv, o[i + 1] * inv);
+        if (A.lse && lane == 0) A.lse[(int64_t(b) * c.nodes + n) * c.heads + h] = none ? neg_inf() : (ref + log2f(sum)) * 0.6931471805599453f;
+    }
 }
 
 }  // namespace spechub

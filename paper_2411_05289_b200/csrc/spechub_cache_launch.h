@@ -8,7 +8,7 @@ namespace spechub {
 
 int launch_append(int dtype, const AppendArgs &a, bool interleaved, cudaStream_t s);
 int launch_accept(const AcceptArgs &a, cudaStream_t s);
-size_t attention_workspace(const CacheArgs &c, int64_t shared_len);
+bool attention_workspace(const CacheArgs &c, int64_t shared_len, size_t *bytes);   // false: more work than a call may have
 int launch_attention(int dtype, const AttentionArgs &a, void *workspace, cudaStream_t s);
 
 }  // namespace spechub

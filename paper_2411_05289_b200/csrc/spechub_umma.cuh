@@ -25,24 +25,18 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
                  : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     return ok != 0;
 }
-__device__ __forceinline__ unsigned long long now_ns() {
-    unsigned long long t;
-    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
-    return t;
-}
+constexpr long long kWaitClocks = 4000000000ll;   // two seconds and more; no wait of a working kernel comes near it
 
-constexpr unsigned long long kWaitNs = 2000000000ull;   // no wait of a working kernel comes near it
-
-// Wait for a phase, for kWaitNs at most.  When a wait runs out, `gave_up` (shared memory) is set; every wait of the CTA then
+// Wait for a phase, for kWaitClocks at most.  When a wait runs out, `gave_up` (shared memory) is set; every wait of the CTA then
 // returns at once, so that the kernel runs to its end (over data that is not valid, within its bounds) and can say so.
 // Called by whole warps, which are together again afterwards.
 __device__ __forceinline__ void bar_wait(uint32_t bar, uint32_t parity, volatile int *gave_up) {
     if (!bar_try(bar, parity)) {
-        const unsigned long long t0 = now_ns();
+        const long long t0 = clock64();
         for (unsigned polls = 1; !bar_try(bar, parity); ++polls) {
             if (polls % 64 != 0) continue;
             if (*gave_up) break;
-            if (now_ns() - t0 > kWaitNs) {
+            if (clock64() - t0 > kWaitClocks) {
                 *gave_up = 1;
                 break;
             }
@@ -96,15 +90,17 @@ __device__ __forceinline__ void tmem_ld32_async(uint32_t taddr, float *v) {
           "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31])
         : "r"(taddr) : "memory");
 }
-__device__ __forceinline__ void tmem_st32_async(uint32_t taddr, const uint32_t *v) {
+__device__ __forceinline__ void tmem_st16_async(uint32_t taddr, const uint32_t *v) {
     asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
-        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
         ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]),
-          "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]),
-          "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]), "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]),
-          "r"(v[30]), "r"(v[31]) : "memory");
+          "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]) : "memory");
 }
-__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// waits for all of this thread's loads; v: what one of them brings (not looked at before)
+__device__ __forceinline__ void tmem_wait_ld32(float *v) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < 32; ++i) asm volatile("" : "+f"(v[i]));
+}
 
 }  // namespace spechub
