@@ -83,6 +83,16 @@ int launch_type(const AttKernelArgs &k, const CUtensorMap &mk, const CUtensorMap
     static bool configured[kMaxDevices] = {};
     const int rc = allow_smem(reinterpret_cast<const void *>(attention_kernel<T, D>), AttShape<D>::kSmem, configured);
     if (rc != SPECHUB_OK) return rc;
+    // the kernel's warps share out kLaunchRegs registers a thread: a build that gives it others must not run
+    static int regs[kMaxDevices] = {};
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return SPECHUB_ERR_LAUNCH;
+    if (regs[dev] == 0) {
+        cudaFuncAttributes fa;
+        if (cudaFuncGetAttributes(&fa, attention_kernel<T, D>) != cudaSuccess) { cudaGetLastError(); return SPECHUB_ERR_LAUNCH; }
+        regs[dev] = fa.numRegs;
+    }
+    if (regs[dev] != kLaunchRegs) return SPECHUB_ERR_LAUNCH;
     const int lrc = launch_grid(attention_kernel<T, D>, k.p.grid, kAttThreads, AttShape<D>::kSmem, 1, s, k, mk, mv);
     if (lrc != SPECHUB_OK) return lrc;
     const int64_t grid = static_cast<int64_t>(k.a.c.batch) * k.a.c.kv_heads * k.p.own_blocks * ((k.p.own_rows + kJoinRows - 1) / kJoinRows) +

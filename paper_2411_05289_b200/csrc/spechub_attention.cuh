@@ -32,6 +32,9 @@ namespace spechub {
 constexpr int kTile = 128;         // keys of a tile, rows of a softmax group
 constexpr int kBlockRows = 256;
 constexpr int kAttThreads = 384;
+// Registers of a thread: what the block is launched with, and how its warpgroups share them then (a row of scores is 128).
+constexpr int kLaunchRegs = 168, kSoftmaxRegs = 200, kOtherRegs = 104;
+static_assert(256 * kSoftmaxRegs + 128 * kOtherRegs <= kAttThreads * kLaunchRegs, "the block's own registers");
 constexpr float kSlack = 8.f;
 // Weights are stored as 2^bias times themselves.  fp16 has numbers down to 2^-24 only: with the reference 7 below, weights of
 // 2^-31 of the largest still count, and the largest is 2^(7 + kSlack) < 65504.
@@ -331,7 +334,158 @@ __global__ void __launch_bounds__(kAttThreads, 1) attention_kernel(const __grid_
     AttWalk walk(K, start);
     AttPiece x = {};
 
-    if (warp == 8) {
+    if (warp < 8) {
+        // ---- softmax ---------------------------------------------------------------------------------
+        more_registers<kSoftmaxRegs>();
+        const int g = warp >> 2, gt = tid & (kTile - 1);
+        const uint32_t lanes = static_cast<uint32_t>(32 * (warp & 3)) << 16;
+        const uint32_t t_s = tm + lanes + L::kS + g * kTile, t_p = tm + lanes + L::kP + g * L::kPStep, t_o = tm + lanes + L::kO;
+        uint32_t s_phase = 0, o_phase = 0;
+        const float cs = A.scale_log2;
+        while (walk.next(x)) {
+            const int row = (x.two ? g * kTile : 0) + gt;
+            const bool warp_on = row - lane < x.rows;   // any row in this warp
+            const AttRow at = row_of(P, x, min(row, x.rows - 1));
+            float ref = neg_inf(), sum = 0.f;
+            const int step = x.two ? 1 : 2, first = x.two ? x.t0 : x.t0 + g;
+            for (int t = first; t < x.t1; t += step) {
+                bar_wait(s_full(g), s_phase, gave_up);
+                s_phase ^= 1u;
+                tmem_fence_after();
+                if (warp_on) {
+                    float s[kTile];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) tmem_ld32_async(t_s + 32 * i, s + 32 * i);
+                    tmem_wait_ld(s);
+                    if (x.masked(t)) {
+                        uint32_t bits[4];
+                        row_bits(A, x, t, at.n, bits);
+#pragma unroll
+                        for (int i = 0; i < kTile; ++i) s[i] = bits[i / 32] >> (i & 31) & 1 ? s[i] : neg_inf();
+                    }
+                    float m0 = neg_inf(), m1 = neg_inf(), m2 = neg_inf(), m3 = neg_inf();
+#pragma unroll
+                    for (int i = 0; i < kTile; i += 8) {
+                        m0 = max3(m0, s[i], s[i + 1]);
+                        m1 = max3(m1, s[i + 2], s[i + 3]);
+                        m2 = max3(m2, s[i + 4], s[i + 5]);
+                        m3 = max3(m3, s[i + 6], s[i + 7]);
+                    }
+                    const float top = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3)) * cs - Weight<T>::kBias;
+                    if (t == first) ref = top;
+                    else if (__any_sync(kFull, top > ref + kSlack && row < x.rows)) {
+                        // (the product that added the last tile to O is done: it was issued before these scores)
+                        const float now = fmaxf(ref, top), f = now == neg_inf() ? 1.f : ex2(ref - now);
+                        sum *= f;
+                        ref = now;
+#pragma unroll 1
+                        for (int i = 0; i < D; i += 32) {
+                            float o[32];
+                            tmem_ld32(t_o + g * D + i, o);
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) o[j] *= f;
+                            tmem_st32(t_o + g * D + i, o);
+                        }
+                    }
+                    const float sub = ref == neg_inf() ? 0.f : -ref;
+                    const float2 cs2 = make_float2(cs, cs), sub2 = make_float2(sub, sub);
+                    float2 l0 = make_float2(0.f, 0.f), l1 = l0;
+#pragma unroll
+                    for (int h = 0; h < 4; ++h) {
+                        uint32_t w[16];
+#pragma unroll
+                        for (int i = 0; i < 16; i += 2) {
+                            const float *y = s + 32 * h + 2 * i;
+                            const float2 a = fma2(make_float2(y[0], y[1]), cs2, sub2), b = fma2(make_float2(y[2], y[3]), cs2, sub2);
+                            const float2 e = make_float2(ex2(a.x), ex2(a.y)), f = make_float2(ex2(b.x), ex2(b.y));
+                            l0 = add2(l0, e);
+                            l1 = add2(l1, f);
+                            w[i] = pack2<T>(e.x, e.y);
+                            w[i + 1] = pack2<T>(f.x, f.y);
+                        }
+                        tmem_st16_async(t_p + 16 * h, w);
+                    }
+                    sum += (l0.x + l0.y) + (l1.x + l1.y);
+                    tmem_wait_st();
+                    tmem_fence_before();
+                }
+                bar_arrive(p_full(g));
+            }
+            // ---- the end of the piece ------------------------------------------------------------------
+            const bool any = first < x.t1;
+            if (any) {
+                bar_wait(o_full(g), o_phase, gave_up);
+                o_phase ^= 1u;
+            }
+            tmem_fence_after();
+            float f0 = 1.f, f1 = 0.f;   // factors of this group's O, of the other group's
+            bool write = warp_on;
+            if (!x.two) {
+                if (g == 1) other[gt] = make_float2(ref, sum);
+                tmem_fence_before();
+                asm volatile("bar.sync 1, 256;" ::: "memory");
+                tmem_fence_after();
+                write = warp_on && g == 0;
+                if (g == 0 && x.t1 - x.t0 > 1) {
+                    const float2 z = other[gt];
+                    const float now = fmaxf(ref, z.x), r = now == neg_inf() ? 0.f : now;
+                    f0 = ex2(ref - r); f1 = ex2(z.x - r);
+                    sum = sum * f0 + z.y * f1;
+                    ref = now;
+                }
+            }
+            if (write) {
+                const bool whole = !x.shared && P.shared_tiles == 0 && x.t1 - x.t0 == x.tiles, join = !x.two && x.t1 - x.t0 > 1;
+                const bool mine = row < x.rows, none = sum == 0.f;
+                const float inv = none ? 0.f : 1.f / sum;
+                const int bad = *static_cast<volatile int *>(&bad_values);
+                int64_t slot_row = 0;
+                if (!whole) {
+                    slot_row = x.shared ? (x.item + int64_t(blockIdx.x)) * P.shared_rows + row
+                                        : P.slots * P.shared_rows + (x.item + int64_t(blockIdx.x)) * P.own_rows + row;
+                    if (mine) P.ml[slot_row] = make_float2(ref, sum);
+                } else if (mine && A.lse) {
+                    A.lse[(static_cast<int64_t>(at.b) * c.nodes + at.n) * c.heads + at.h] = none ? neg_inf() : (ref + log2f(sum)) * 0.6931471805599453f;
+                }
+#pragma unroll 1
+                for (int i = 0; i < D; i += 32) {
+                    float o[32];
+                    tmem_ld32(t_o + g * D + i, o);
+                    if (join) {
+                        float z[32];
+                        tmem_ld32(t_o + D + i, z);
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) o[j] = o[j] * f0 + z[j] * f1;
+                    }
+                    if (bad && !x.shared && mine) {
+                        float z[32];
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) z[j] = o[j];
+                        add_not_finite<T>(A, x, at.n, i, z);
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) o[j] = z[j];
+                    }
+                    if (mine && whole) {
+                        T *dst = static_cast<T *>(A.out.data) + at.b * A.out.seq + at.n * A.out.node + at.h * A.out.head + i;
+#pragma unroll
+                        for (int j = 0; j < 32; j += 8) {
+                            uint4 u;
+                            u.x = pack2<T>(o[j] * inv, o[j + 1] * inv); u.y = pack2<T>(o[j + 2] * inv, o[j + 3] * inv);
+                            u.z = pack2<T>(o[j + 4] * inv, o[j + 5] * inv); u.w = pack2<T>(o[j + 6] * inv, o[j + 7] * inv);
+                            *reinterpret_cast<uint4 *>(dst + j) = u;
+                        }
+                    } else if (mine) {
+                        float *dst = P.o + slot_row * D + i;
+#pragma unroll
+                        for (int j = 0; j < 32; j += 4) *reinterpret_cast<float4 *>(dst + j) = make_float4(o[j], o[j + 1], o[j + 2], o[j + 3]);
+                    }
+                    __syncwarp();
+                }
+            }
+            tmem_fence_before();
+            bar_arrive(o_free);
+        }
+    } else if (fewer_registers<kOtherRegs>(), warp == 8) {
         // ---- K and V tiles -------------------------------------------------------------------------
         int stage = 0;
         uint32_t phase = 0;
@@ -391,11 +545,11 @@ __global__ void __launch_bounds__(kAttThreads, 1) attention_kernel(const __grid_
         };
         const auto scores = [&](int t, int q, int s) {   // S_t = Q_q K^T
             if (lane != 0) return;
+            const uint32_t a = operand(s_q + q * L::kTileBytes, 16), b = operand(s_kv + s * L::kTileBytes, 16), d = tm + L::kS + t * kTile;
 #pragma unroll
             for (int k = 0; k < D / 16; ++k) {
-                const uint32_t off = (k / 4) * L::kHalfBytes + (k % 4) * 32;
-                mma_ss(tm + L::kS + t * kTile, smem_desc(s_q + q * L::kTileBytes + off, 16, 1024), smem_desc(s_kv + s * L::kTileBytes + off, 16, 1024),
-                       desc_s, k > 0);
+                const uint32_t off = ((k / 4) * L::kHalfBytes + (k % 4) * 32) >> 4;
+                mma_ss(d, a + off, b + off, desc_s, k > 0);
             }
             mma_commit(s_full(t));
         };
@@ -404,10 +558,9 @@ __global__ void __launch_bounds__(kAttThreads, 1) attention_kernel(const __grid_
             p_phase[t] ^= 1u;
             tmem_fence_after();
             if (lane != 0) return;
+            const uint32_t a = tm + L::kP + t * L::kPStep, b = operand(s_kv + s * L::kTileBytes, L::kHalfBytes), d = tm + L::kO + t * D;
 #pragma unroll
-            for (int k = 0; k < kTile / 16; ++k)
-                mma_ts(tm + L::kO + t * D, tm + L::kP + t * L::kPStep + 8 * k, smem_desc(s_kv + s * L::kTileBytes + k * 2048, L::kHalfBytes, 1024), desc_o,
-                       add || k > 0);
+            for (int k = 0; k < kTile / 16; ++k) mma_ts(d, a + 8 * k, b + k * (2048 >> 4), desc_o, add || k > 0);
         };
         // values behind the end, and those of tree nodes that are no numbers: zero
         const auto clear = [&](int tile, int s) {
@@ -505,7 +658,7 @@ __global__ void __launch_bounds__(kAttThreads, 1) attention_kernel(const __grid_
         bar_wait(o_free, free_phase, gave_up);
     } else if (warp >= 10) {
         // ---- queries -----------------------------------------------------------------------------------
-        constexpr int kVecs = D / 8, kStep = 64 / kVecs, kBatch = 16;   // rows that the two warps bring at once; loads in flight per thread
+        constexpr int kVecs = D / 8, kStep = 64 / kVecs, kBatch = 8;   // rows that the two warps bring at once; loads in flight per thread
         int slot = 0;
         uint32_t phase = 1;
         const int qt = tid - 320, vec = qt % kVecs;
@@ -535,166 +688,6 @@ __global__ void __launch_bounds__(kAttThreads, 1) attention_kernel(const __grid_
         for (int i = 0; i < 2; ++i) {
             bar_wait(q_empty(slot), phase, gave_up);
             if (++slot == 2) { slot = 0; phase ^= 1u; }
-        }
-    } else if (warp < 8) {
-        // ---- softmax ---------------------------------------------------------------------------------
-        const int g = warp >> 2, gt = tid & (kTile - 1);
-        const uint32_t lanes = static_cast<uint32_t>(32 * (warp & 3)) << 16;
-        const uint32_t t_s = tm + lanes + L::kS + g * kTile, t_p = tm + lanes + L::kP + g * L::kPStep, t_o = tm + lanes + L::kO;
-        uint32_t s_phase = 0, o_phase = 0;
-        const float cs = A.scale_log2;
-        while (walk.next(x)) {
-            const int row = (x.two ? g * kTile : 0) + gt;
-            const bool warp_on = row - lane < x.rows;   // any row in this warp
-            const AttRow at = row_of(P, x, min(row, x.rows - 1));
-            float ref = neg_inf(), sum = 0.f;
-            const int step = x.two ? 1 : 2, first = x.two ? x.t0 : x.t0 + g;
-            for (int t = first; t < x.t1; t += step) {
-                bar_wait(s_full(g), s_phase, gave_up);
-                s_phase ^= 1u;
-                tmem_fence_after();
-                if (warp_on) {
-                    // twice through the scores, 32 at a time (a row of 128 would not fit the registers): maximum, weights
-                    const bool masked = x.masked(t);
-                    uint32_t bits[4] = {~0u, ~0u, ~0u, ~0u};
-                    if (masked) row_bits(A, x, t, at.n, bits);
-                    float s[2][32], m0 = neg_inf(), m1 = neg_inf(), m2 = neg_inf(), m3 = neg_inf();
-                    const auto hide = [&](float *y, uint32_t b) {
-                        if (masked) {
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) y[i] = b >> i & 1 ? y[i] : neg_inf();
-                        }
-                    };
-                    tmem_ld32_async(t_s, s[0]);
-#pragma unroll
-                    for (int h = 0; h < 4; ++h) {
-                        float *y = s[h & 1];
-                        tmem_wait_ld32(y);
-                        if (h < 3) tmem_ld32_async(t_s + 32 * (h + 1), s[~h & 1]);
-                        hide(y, bits[h]);
-#pragma unroll
-                        for (int i = 0; i < 32; i += 8) {
-                            m0 = fmaxf(m0, fmaxf(y[i], y[i + 1]));
-                            m1 = fmaxf(m1, fmaxf(y[i + 2], y[i + 3]));
-                            m2 = fmaxf(m2, fmaxf(y[i + 4], y[i + 5]));
-                            m3 = fmaxf(m3, fmaxf(y[i + 6], y[i + 7]));
-                        }
-                    }
-                    const float top = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3)) * cs - Weight<T>::kBias;
-                    if (t == first) ref = top;
-                    else if (__any_sync(kFull, top > ref + kSlack && row < x.rows)) {
-                        // (the product that added the last tile to O is done: it was issued before these scores)
-                        const float now = fmaxf(ref, top), f = now == neg_inf() ? 1.f : ex2(ref - now);
-                        sum *= f;
-                        ref = now;
-#pragma unroll 1
-                        for (int i = 0; i < D; i += 32) {
-                            float o[32];
-                            tmem_ld32(t_o + g * D + i, o);
-#pragma unroll
-                            for (int j = 0; j < 32; ++j) o[j] *= f;
-                            tmem_st32(t_o + g * D + i, o);
-                        }
-                    }
-                    tmem_ld32_async(t_s, s[0]);
-                    const float sub = ref == neg_inf() ? 0.f : -ref;
-                    float l0 = 0.f, l1 = 0.f, l2 = 0.f, l3 = 0.f;
-#pragma unroll
-                    for (int h = 0; h < 4; ++h) {
-                        float *y = s[h & 1];
-                        uint32_t w[16];
-                        tmem_wait_ld32(y);
-                        if (h < 3) tmem_ld32_async(t_s + 32 * (h + 1), s[~h & 1]);
-                        hide(y, bits[h]);
-#pragma unroll
-                        for (int i = 0; i < 32; i += 4) {
-                            const float a = ex2(fmaf(y[i], cs, sub)), b = ex2(fmaf(y[i + 1], cs, sub));
-                            const float e = ex2(fmaf(y[i + 2], cs, sub)), f = ex2(fmaf(y[i + 3], cs, sub));
-                            l0 += a; l1 += b; l2 += e; l3 += f;
-                            w[i / 2] = pack2<T>(a, b);
-                            w[i / 2 + 1] = pack2<T>(e, f);
-                        }
-                        tmem_st16_async(t_p + 16 * h, w);   // (over scores that all have been read)
-                    }
-                    sum += (l0 + l1) + (l2 + l3);
-                    tmem_wait_st();
-                    tmem_fence_before();
-                }
-                bar_arrive(p_full(g));
-            }
-            // ---- the end of the piece ------------------------------------------------------------------
-            const bool any = first < x.t1;
-            if (any) {
-                bar_wait(o_full(g), o_phase, gave_up);
-                o_phase ^= 1u;
-            }
-            tmem_fence_after();
-            float f0 = 1.f, f1 = 0.f;   // factors of this group's O, of the other group's
-            bool write = warp_on;
-            if (!x.two) {
-                if (g == 1) other[gt] = make_float2(ref, sum);
-                tmem_fence_before();
-                asm volatile("bar.sync 1, 256;" ::: "memory");
-                tmem_fence_after();
-                write = warp_on && g == 0;
-                if (g == 0 && x.t1 - x.t0 > 1) {
-                    const float2 z = other[gt];
-                    const float now = fmaxf(ref, z.x), r = now == neg_inf() ? 0.f : now;
-                    f0 = ex2(ref - r); f1 = ex2(z.x - r);
-                    sum = sum * f0 + z.y * f1;
-                    ref = now;
-                }
-            }
-            if (write) {
-                const bool whole = !x.shared && P.shared_tiles == 0 && x.t1 - x.t0 == x.tiles, join = !x.two && x.t1 - x.t0 > 1;
-                const bool mine = row < x.rows, none = sum == 0.f;
-                const float inv = none ? 0.f : 1.f / sum;
-                const int bad = *static_cast<volatile int *>(&bad_values);
-                int64_t slot_row = 0;
-                if (!whole) {
-                    slot_row = x.shared ? (x.item + int64_t(blockIdx.x)) * P.shared_rows + row
-                                        : P.slots * P.shared_rows + (x.item + int64_t(blockIdx.x)) * P.own_rows + row;
-                    if (mine) P.ml[slot_row] = make_float2(ref, sum);
-                } else if (mine && A.lse) {
-                    A.lse[(static_cast<int64_t>(at.b) * c.nodes + at.n) * c.heads + at.h] = none ? neg_inf() : (ref + log2f(sum)) * 0.6931471805599453f;
-                }
-#pragma unroll 1
-                for (int i = 0; i < D; i += 32) {
-                    float o[32];
-                    tmem_ld32(t_o + g * D + i, o);
-                    if (join) {
-                        float z[32];
-                        tmem_ld32(t_o + D + i, z);
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) o[j] = o[j] * f0 + z[j] * f1;
-                    }
-                    if (bad && !x.shared && mine) {
-                        float z[32];
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) z[j] = o[j];
-                        add_not_finite<T>(A, x, at.n, i, z);
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) o[j] = z[j];
-                    }
-                    if (mine && whole) {
-                        T *dst = static_cast<T *>(A.out.data) + at.b * A.out.seq + at.n * A.out.node + at.h * A.out.head + i;
-#pragma unroll
-                        for (int j = 0; j < 32; j += 8) {
-                            uint4 u;
-                            u.x = pack2<T>(o[j] * inv, o[j + 1] * inv); u.y = pack2<T>(o[j + 2] * inv, o[j + 3] * inv);
-                            u.z = pack2<T>(o[j + 4] * inv, o[j + 5] * inv); u.w = pack2<T>(o[j + 6] * inv, o[j + 7] * inv);
-                            *reinterpret_cast<uint4 *>(dst + j) = u;
-                        }
-                    } else if (mine) {
-                        float *dst = P.o + slot_row * D + i;
-#pragma unroll
-                        for (int j = 0; j < 32; j += 4) *reinterpret_cast<float4 *>(dst + j) = make_float4(o[j], o[j + 1], o[j + 2], o[j + 3]);
-                    }
-                    __syncwarp();
-                }
-            }
-            tmem_fence_before();
-            bar_arrive(o_free);
         }
     }
     tmem_fence_before();

@@ -54,25 +54,25 @@ __device__ __forceinline__ void tma_prefetch_map(const CUtensorMap *map) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
 }
 
-// Operand in shared memory, rows of 128 bytes, swizzled by 128 bytes (eight rows of 1024 bytes repeat).  `sbo`: bytes between
-// groups of eight rows; `lbo`: bytes between blocks of 64 elements along the axis that lies in a row (operands whose rows run
-// along M or N; not used by those whose rows run along K).
-__device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t lbo, uint32_t sbo) {
-    return (static_cast<uint64_t>(2) << 61) | (static_cast<uint64_t>(1) << 46) | (static_cast<uint64_t>(sbo >> 4) << 32) |
-           (static_cast<uint64_t>((lbo >> 4) & 0x3fff) << 16) | ((addr >> 4) & 0x3fff);
-}
+// Operand in shared memory, rows of 128 bytes, swizzled by 128 bytes (eight rows of 1024 bytes repeat, and groups of eight rows follow
+// each other): the low word of its descriptor.  `lbo`: bytes between blocks of 64 elements along the axis that lies in a row (operands
+// whose rows run along M or N; not used by those whose rows run along K).  16 further bytes are one more.
+__device__ __forceinline__ uint32_t operand(uint32_t addr, uint32_t lbo) { return (lbo >> 4 << 16) | addr >> 4; }
+constexpr uint32_t kOperandHigh = 2u << 29 | 1u << 14 | 1024u >> 4;
 // M = 128, fp32 accumulator, both operands bf16 or both fp16
 __host__ __device__ constexpr uint32_t mma_desc(bool bf16, int n, bool b_rows_along_n) {
     return (1u << 4) | (bf16 ? (1u << 7) | (1u << 10) : 0u) | (b_rows_along_n ? 1u << 16 : 0u) | (static_cast<uint32_t>(n / 8) << 17) | (8u << 24);
 }
 // d (tensor memory, 128 x n) = a b (+ d), 16 elements of K; one thread issues
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t desc, bool add) {
-    asm volatile("{ .reg .pred p; setp.ne.u32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p; }"
-                 ::"r"(d), "l"(a), "l"(b), "r"(desc), "r"(static_cast<uint32_t>(add)) : "memory");
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t desc, bool add) {
+    asm volatile("{ .reg .pred p; .reg .b64 x, y; mov.b64 x, {%1, %5}; mov.b64 y, {%2, %5}; setp.ne.u32 p, %4, 0; "
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, p; }"
+                 ::"r"(d), "r"(a), "r"(b), "r"(desc), "r"(static_cast<uint32_t>(add)), "r"(kOperandHigh) : "memory");
 }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t desc, bool add) {   // a in tensor memory
-    asm volatile("{ .reg .pred p; setp.ne.u32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p; }"
-                 ::"r"(d), "r"(a), "l"(b), "r"(desc), "r"(static_cast<uint32_t>(add)) : "memory");
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t desc, bool add) {   // a in tensor memory
+    asm volatile("{ .reg .pred p; .reg .b64 y; mov.b64 y, {%2, %5}; setp.ne.u32 p, %4, 0; "
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %3, p; }"
+                 ::"r"(d), "r"(a), "r"(b), "r"(desc), "r"(static_cast<uint32_t>(add)), "r"(kOperandHigh) : "memory");
 }
 // the barrier gets an arrival when everything that this thread has issued to the tensor core is done
 __device__ __forceinline__ void mma_commit(uint32_t bar) {
@@ -96,11 +96,34 @@ __device__ __forceinline__ void tmem_st16_async(uint32_t taddr, const uint32_t *
         ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]),
           "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]) : "memory");
 }
-// waits for all of this thread's loads; v: what one of them brings (not looked at before)
-__device__ __forceinline__ void tmem_wait_ld32(float *v) {
+// waits for all of this thread's loads; v: what they bring (not looked at before)
+template <int N> __device__ __forceinline__ void tmem_wait_ld(float (&v)[N]) {
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
-    for (int i = 0; i < 32; ++i) asm volatile("" : "+f"(v[i]));
+    for (int i = 0; i < N; ++i) asm volatile("" : "+f"(v[i]));
+}
+
+// How the warpgroups of a block share its registers; at the beginning of what a role alone does.
+template <int N> __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N> __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+
+// two at once
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 d;
+    asm("{ .reg .b64 x, y, z; mov.b64 x, {%2, %3}; mov.b64 y, {%4, %5}; mov.b64 z, {%6, %7}; fma.rn.f32x2 x, x, y, z; mov.b64 {%0, %1}, x; }"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    float2 d;
+    asm("{ .reg .b64 x, y; mov.b64 x, {%2, %3}; mov.b64 y, {%4, %5}; add.rn.f32x2 x, x, y; mov.b64 {%0, %1}, x; }"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {   // (a NaN is not taken)
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
 }
 
 }  // namespace spechub
