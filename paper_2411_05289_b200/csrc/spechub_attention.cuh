@@ -534,7 +534,7 @@ __global__ void __launch_bounds__(kAttThreads, 1) attention_kernel(const __grid_
     } else if (warp == 9) {
         // ---- matrix instructions -------------------------------------------------------------------
         int stage = 0;
-        uint32_t phase = 0, q_phase = 0, p_phase[2] = {0, 0}, free_phase = 1;
+        uint32_t phase = 0, q_phase = 0, p_phase = 0, free_phase = 1;
         int q_slot = 0;
         constexpr uint32_t desc_s = mma_desc(kBf16, kTile, false), desc_o = mma_desc(kBf16, D, true);
         const auto arrived = [&]() {   // the next stage of the ring
@@ -543,24 +543,33 @@ __global__ void __launch_bounds__(kAttThreads, 1) attention_kernel(const __grid_
             if (++stage == L::kStages) { stage = 0; phase ^= 1u; }
             return s;
         };
+        const bool lead = lane == 0;
+        const uint32_t tmu = uniform(tm), kv_op = operand(uniform(s_kv), L::kHalfBytes), q_op = operand(uniform(s_q), L::kHalfBytes);
         const auto scores = [&](int t, int q, int s) {   // S_t = Q_q K^T
-            if (lane != 0) return;
-            const uint32_t a = operand(s_q + q * L::kTileBytes, 16), b = operand(s_kv + s * L::kTileBytes, 16), d = tm + L::kS + t * kTile;
+            uint32_t a = uniform(q_op + q * (L::kTileBytes >> 4)), b = uniform(kv_op + s * (L::kTileBytes >> 4));
+            const uint32_t d = uniform(tmu + L::kS + t * kTile);
+#pragma unroll 1
+            for (int h = 0; h < L::kHalves; ++h) {
 #pragma unroll
-            for (int k = 0; k < D / 16; ++k) {
-                const uint32_t off = ((k / 4) * L::kHalfBytes + (k % 4) * 32) >> 4;
-                mma_ss(d, a + off, b + off, desc_s, k > 0);
+                for (int k = 0; k < 4; ++k) mma_ss(d, a + 2 * k, b + 2 * k, desc_s, h + k > 0, lead);
+                a += L::kHalfBytes >> 4;
+                b += L::kHalfBytes >> 4;
             }
-            mma_commit(s_full(t));
+            mma_commit(s_full(t), lead);
         };
         const auto products = [&](int t, int s, bool add) {   // O_t (+)= P_t V
-            bar_wait(p_full(t), p_phase[t], gave_up);
-            p_phase[t] ^= 1u;
+            uint32_t a = uniform(tmu + L::kP + t * L::kPStep), b = uniform(kv_op + s * (L::kTileBytes >> 4));
+            const uint32_t d = uniform(tmu + L::kO + t * D);
+            bar_wait(p_full(t), p_phase >> t & 1u, gave_up);
+            p_phase ^= 1u << t;
             tmem_fence_after();
-            if (lane != 0) return;
-            const uint32_t a = tm + L::kP + t * L::kPStep, b = operand(s_kv + s * L::kTileBytes, L::kHalfBytes), d = tm + L::kO + t * D;
+#pragma unroll 1
+            for (int h = 0; h < 2; ++h) {
 #pragma unroll
-            for (int k = 0; k < kTile / 16; ++k) mma_ts(d, a + 8 * k, b + k * (2048 >> 4), desc_o, add || k > 0);
+                for (int k = 0; k < 4; ++k) mma_ts(d, a + 8 * k, b + k * (2048 >> 4), desc_o, add || h + k > 0, lead);
+                a += 32;
+                b += 4 * (2048 >> 4);
+            }
         };
         // values behind the end, and those of tree nodes that are no numbers: zero
         const auto clear = [&](int tile, int s) {
@@ -599,59 +608,49 @@ __global__ void __launch_bounds__(kAttThreads, 1) attention_kernel(const __grid_
             __syncwarp();
         };
         while (walk.next(x)) {
-            // queries of both groups, or of one block in whichever slot is next
-            int q[2];
-            for (int i = 0; i < (x.two ? 2 : 1); ++i) {
-                q[i] = q_slot;
+            // Queries of both groups, or of one block in whichever slot is next.
+            int q0 = q_slot, q1;
+            bar_wait(q_full(q_slot), q_phase, gave_up);
+            if (++q_slot == 2) { q_slot = 0; q_phase ^= 1u; }
+            q1 = x.two ? q_slot : q0;
+            if (x.two) {
                 bar_wait(q_full(q_slot), q_phase, gave_up);
                 if (++q_slot == 2) { q_slot = 0; q_phase ^= 1u; }
             }
+            // Products of tile t, scores of tile t + ahead: each once in the code, which other warps push out of the instruction cache.
             const int ahead = x.two ? 1 : 2;
-            const auto last_scores = [&](int t) {   // after those of tile t: is a slot of queries free?
-                if (t == x.t1 - 1 && lane == 0) {
-                    mma_commit(q_empty(q[0]));
-                    if (x.two) mma_commit(q_empty(q[1]));
+            for (int t = x.t0 - ahead; t < x.t1; ++t) {
+                const bool now = t >= x.t0, more = t + ahead < x.t1;
+                int v = 0, s = 0;
+                if (t == x.t0) {   // O of the piece before has been read by now or soon, and what was said of its values
+                    bar_wait(o_free, free_phase, gave_up);
+                    free_phase ^= 1u;
+                    tmem_fence_after();
+                    if (lane == 0) *static_cast<volatile int *>(&bad_values) = 0;
+                    __syncwarp();
                 }
-            };
-            for (int i = 0; i < ahead && x.t0 + i < x.t1; ++i) {
-                const int s = arrived();
-                scores(i, q[0], s);
-                if (x.two) scores(1, q[1], s);
-                if (lane == 0) mma_commit(kv_empty(s));
-                last_scores(x.t0 + i);
-            }
-            // O of the piece before has been read by now or soon, and what was said of its values
-            bar_wait(o_free, free_phase, gave_up);
-            free_phase ^= 1u;
-            tmem_fence_after();
-            if (lane == 0) *static_cast<volatile int *>(&bad_values) = 0;
-            __syncwarp();
-            for (int t = x.t0; t < x.t1; ++t) {
-                const int v = arrived();
-                if (x.masked(t)) clear(t, v);
-                const bool more = t + ahead < x.t1;
-                if (x.two) {
-                    const int s = more ? arrived() : 0;
-                    for (int g = 0; g < 2; ++g) {
-                        products(g, v, t > x.t0);
-                        if (more) scores(g, q[g], s);
-                        else if (lane == 0) mma_commit(o_full(g));
+                if (now) {
+                    v = arrived();
+                    if (x.masked(t)) clear(t, v);
+                }
+                const int g0 = x.two ? 0 : (t + ahead - x.t0) & 1, g1 = x.two ? 2 : g0 + 1;
+                for (int g = g0; g < g1; ++g) {
+                    if (now) {
+                        products(g, v, t >= x.t0 + ahead);
+                        if (g == g1 - 1) mma_commit(kv_empty(v), lead);
                     }
-                    if (lane == 0) {
-                        mma_commit(kv_empty(v));
-                        if (more) mma_commit(kv_empty(s));
-                    }
-                } else {
-                    const int g = (t - x.t0) & 1;
-                    products(g, v, t >= x.t0 + 2);
-                    if (lane == 0) mma_commit(kv_empty(v));
                     if (more) {
-                        const int s = arrived();
-                        scores(g, q[0], s);
-                        if (lane == 0) mma_commit(kv_empty(s));
-                    } else if (lane == 0) mma_commit(o_full(g));
+                        if (g == g0) s = arrived();
+                        scores(g, g ? q1 : q0, s);
+                        if (g == g1 - 1) {
+                            mma_commit(kv_empty(s), lead);
+                            if (t + ahead == x.t1 - 1) {   // the last ones
+                                mma_commit(q_empty(q0), lead);
+                                if (x.two) mma_commit(q_empty(q1), lead);
+                            }
+                        }
+                    } else if (now) mma_commit(o_full(g), lead);
                 }
-                if (more) last_scores(t + ahead);
             }
         }
         // (the last arrivals come before the CTA ends)

@@ -63,21 +63,24 @@ constexpr uint32_t kOperandHigh = 2u << 29 | 1u << 14 | 1024u >> 4;
 __host__ __device__ constexpr uint32_t mma_desc(bool bf16, int n, bool b_rows_along_n) {
     return (1u << 4) | (bf16 ? (1u << 7) | (1u << 10) : 0u) | (b_rows_along_n ? 1u << 16 : 0u) | (static_cast<uint32_t>(n / 8) << 17) | (8u << 24);
 }
-// d (tensor memory, 128 x n) = a b (+ d), 16 elements of K; one thread issues
-__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t desc, bool add) {
-    asm volatile("{ .reg .pred p; .reg .b64 x, y; mov.b64 x, {%1, %5}; mov.b64 y, {%2, %5}; setp.ne.u32 p, %4, 0; "
-                 "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, p; }"
-                 ::"r"(d), "r"(a), "r"(b), "r"(desc), "r"(static_cast<uint32_t>(add)), "r"(kOperandHigh) : "memory");
+// d (tensor memory, 128 x n) = a b (+ d), 16 elements of K.  The whole warp comes here, with the same values, and the one thread for
+// which `lead` holds issues: without a branch around it the operands stay in uniform registers (100 -> 64 clocks per instruction).
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t desc, bool add, bool lead) {
+    asm volatile("{ .reg .pred p, q; .reg .b64 x, y; mov.b64 x, {%1, %5}; mov.b64 y, {%2, %5}; setp.ne.u32 p, %4, 0; setp.ne.u32 q, %6, 0; "
+                 "@q tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, p; }"
+                 ::"r"(d), "r"(a), "r"(b), "r"(desc), "r"(static_cast<uint32_t>(add)), "r"(kOperandHigh), "r"(static_cast<uint32_t>(lead)) : "memory");
 }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t desc, bool add) {   // a in tensor memory
-    asm volatile("{ .reg .pred p; .reg .b64 y; mov.b64 y, {%2, %5}; setp.ne.u32 p, %4, 0; "
-                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %3, p; }"
-                 ::"r"(d), "r"(a), "r"(b), "r"(desc), "r"(static_cast<uint32_t>(add)), "r"(kOperandHigh) : "memory");
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t desc, bool add, bool lead) {   // a in tensor memory
+    asm volatile("{ .reg .pred p, q; .reg .b64 y; mov.b64 y, {%2, %5}; setp.ne.u32 p, %4, 0; setp.ne.u32 q, %6, 0; "
+                 "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %3, p; }"
+                 ::"r"(d), "r"(a), "r"(b), "r"(desc), "r"(static_cast<uint32_t>(add)), "r"(kOperandHigh), "r"(static_cast<uint32_t>(lead)) : "memory");
 }
 // the barrier gets an arrival when everything that this thread has issued to the tensor core is done
-__device__ __forceinline__ void mma_commit(uint32_t bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+__device__ __forceinline__ void mma_commit(uint32_t bar, bool lead) {
+    asm volatile("{ .reg .pred q; setp.ne.u32 q, %1, 0; @q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0]; }"
+                 ::"r"(bar), "r"(static_cast<uint32_t>(lead)) : "memory");
 }
+__device__ __forceinline__ int uniform(int v) { return __shfl_sync(kFull, v, 0); }   // says so to the compiler
 
 // 32 columns of the warp's 32 lanes, not waited for
 __device__ __forceinline__ void tmem_ld32_async(uint32_t taddr, float *v) {
