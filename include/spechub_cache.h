@@ -60,6 +60,7 @@ extern "C" {
 
 /* element type of the cache (SPECHUB_BF16 is the other one) */
 #define SPECHUB_F16 2
+#define SPECHUB_MAX_GROUP 128 /* most query heads per cache head that spechub_tree_attention takes */
 
 #define SPECHUB_ERR_ALIGN (-11)  /* a pointer or stride is not a multiple of 16 bytes, or rows of an output or of the cache overlap */
 #define SPECHUB_ERR_CACHE (-12)  /* bad cache or head shape: see spechub_cache_desc */

@@ -18,8 +18,8 @@ int check_cache_desc(const spechub_cache_desc *d) {
         d->table_width < 1)
         return SPECHUB_ERR_CACHE;
     if (static_cast<int64_t>(d->batch) * d->nodes > 0x7fffffffLL / d->heads) return SPECHUB_ERR_SHAPE;
-    // slots are counted in 32 bits where a sequence's keys are
-    if ((static_cast<int64_t>(d->table_width) + 1) * d->page_size > 0x7fffffffLL) return SPECHUB_ERR_CACHE;
+    // a sequence's slots, and those of the tile behind them, are counted in 31 bits
+    if (static_cast<int64_t>(d->table_width) * d->page_size > 0x7ffff000LL) return SPECHUB_ERR_CACHE;
     if (d->batch > 1 && d->stride_table < d->table_width) return SPECHUB_ERR_STRIDE;
     return SPECHUB_OK;
 }
@@ -117,7 +117,7 @@ int spechub_tree_attention(const spechub_cache_desc *desc, const spechub_heads *
                            size_t workspace_bytes, void *stream) {
     int rc = check_cache_desc(desc);
     if (rc != SPECHUB_OK) return rc;
-    if (desc->layers != 1) return SPECHUB_ERR_CACHE;
+    if (desc->layers != 1 || desc->heads / desc->kv_heads > SPECHUB_MAX_GROUP) return SPECHUB_ERR_CACHE;
     if (!(scale > 0.f && isfinite(scale))) return SPECHUB_ERR_SCALE;
     if (shared_len < 0 || shared_len > 0x3fffffffLL || shared_width < 0 || shared_len > static_cast<int64_t>(shared_width) * desc->page_size)
         return SPECHUB_ERR_SHARED;
@@ -126,7 +126,7 @@ int spechub_tree_attention(const spechub_cache_desc *desc, const spechub_heads *
     if (desc->batch == 0) return SPECHUB_OK;
     AttentionArgs a = {};
     rc = cache_args(desc, k_cache, v_cache, status, &a.c);
-    if (rc == SPECHUB_OK) rc = heads_of(q, desc, desc->heads, false, &a.q);
+    if (rc == SPECHUB_OK) rc = heads_of(q, desc, desc->heads, true, &a.q);   // (rows of a tensor copy lie apart)
     if (rc == SPECHUB_OK) rc = heads_of(out, desc, desc->heads, true, &a.out);
     if (rc != SPECHUB_OK) return rc;
     if (!mask || (shared_len > 0 && !shared_table)) return SPECHUB_ERR_NULL;

@@ -12,15 +12,17 @@
 // the lengths alone.  So a few long sequences are split as finely as many short ones are gathered.  A run that covers a block's tiles
 // is finished in place; other pieces go to the workspace and attention_join_kernel adds them in the order of the CTAs.
 //
-// CTA.  Warp 8 brings K and V tiles through a ring of bulk tensor copies (a box per page and 64 dimensions), warp 9 issues the
-// matrix instructions, warps 0-3 and 4-7 are two softmax groups, a row per thread, each with its own S, P and O in tensor memory.
-// More than 128 rows: each group has 128 of them and every K / V tile serves both.  Up to 128 rows: the groups take the tiles in turn,
-// for the same rows, and are joined at the end of the piece; else the tensor core and the loads would wait while one group computes.
-// P takes the place of S (head_dim 64 has room for its own).
+// CTA.  Warp 8 brings queries and keys, warp 11 values (bulk tensor copies, a box per page and 64 dimensions, each through a ring of its
+// own), one thread of warp 9 issues the matrix instructions, warps 0-3 and 4-7 are two softmax groups, a row per thread, each with its
+// own S, P and O in tensor memory.  Two tiles of 128 rows: each group has one of them and every K / V tile serves both.  One: the groups
+// take the K / V tiles in turn, for the same rows, and are joined at the end of the piece; else the tensor core and the loads would
+// wait while one group computes.  P takes the place of S (head_dim 64 has room for its own).  A single warp gets through an instruction
+// in 4 to 5 clocks, so what the single warps and the turnover between pieces do is kept short: queries and outputs are copied as tensors
+// too (a box of all heads of some nodes), pieces of the workspace as they lie in shared memory, and the next piece is looked up early.
 //
 // What lies behind a sequence's end in a page may be anything.  Its scores are replaced, and its values, and values of tree nodes
-// that are no finite numbers, are cleared in shared memory before the product, since 0 * NaN would reach every row; the rows that do see
-// such a node get it added at the end.
+// that are no finite numbers, are cleared in shared memory before the product (by warp 10), since 0 * NaN would reach every row; the
+// rows that do see such a node get it added at the end.
 #pragma once
 
 #include "spechub_pages.cuh"
@@ -30,7 +32,6 @@
 namespace spechub {
 
 constexpr int kTile = 128;         // keys of a tile, rows of a softmax group
-constexpr int kBlockRows = 256;
 constexpr int kAttThreads = 384;
 // Registers of a thread: what the block is launched with, and how its warpgroups share them then (a row of scores is 128).
 constexpr int kLaunchRegs = 168, kSoftmaxRegs = 200, kOtherRegs = 104;
@@ -47,8 +48,10 @@ struct AttShape {
     static constexpr int kHalves = D / 64;
     static constexpr int kHalfBytes = kTile * 128;                   // 128 rows of 64 elements
     static constexpr int kTileBytes = kHalves * kHalfBytes;          // a tile of keys, of values, or of queries
-    static constexpr int kStages = 160 * 1024 / kTileBytes;
-    static constexpr int kSmem = (2 + kStages) * kTileBytes + 1024;  // (1024: alignment)
+    static constexpr int kKeyStages = D == 64 ? 5 : 2, kValueStages = D == 64 ? 5 : 3;
+    // Outputs leave through 4 KB per softmax warp: for heads of 128 in the place of the piece's queries, which are 32 KB a tile.
+    static constexpr int kStaging = D == 64 ? 8 * 4096 : 0;
+    static constexpr int kSmem = (2 + kKeyStages + kValueStages) * kTileBytes + kStaging + 1024;  // (1024: alignment)
     // columns of tensor memory
     static constexpr int kS = 0, kO = 256, kP = D == 64 ? 384 : 0, kPStep = D == 64 ? 64 : 128;
 };
@@ -67,22 +70,32 @@ struct FastDiv {
 // What the host knows of the work.  A block of `tiles` tiles costs kBlockCost + tiles * (shared_cost or own_cost), and the CTAs share
 // the sum of the costs evenly.
 constexpr int kBlockCost = 6, kTileCost = 4;
+
+// Rows in tiles.  A tile is `nodes` nodes (all query heads of a cache head), at most 128 rows.  `parts` tiles follow each other within
+// `period` nodes, then the next period begins: the nodes of one sequence, or (parts = 1, period = nodes) of the batch as it goes on.
+struct AttRows {
+    int nodes, parts, period, tiles, blocks;   // blocks of two tiles, per cache head
+    int slot_tiles, slot_rows;                 // of a block in the workspace: tiles, and rows of each
+    FastDiv by_nodes, by_period, by_parts;
+};
 struct AttPlan {
-    int shared_tiles, shared_blocks, own_blocks, grid;   // tiles of the prefix; row blocks per cache head: of all rows, of a sequence
-    int shared_rows, own_rows;                           // rows of a slot in the workspace
-    int shared_items, shared_cost;                       // blocks of the prefix, what they cost
-    int64_t slots;                                       // slots of the shared pieces
-    FastDiv group, nodes;
-    int *before;                                         // [batch + 1] cost of the own blocks before sequence b
-    int *error;                                          // [grid]
-    float2 *ml;                                          // (reference, sum) of every row of every slot
-    float *o;                                            // [..][head_dim], not divided by the sum
+    AttRows own, shared;          // a sequence's rows; the batch's
+    int shared_tiles, grid;       // tiles of keys of the prefix
+    int shared_cost;
+    int64_t shared_slots;
+    bool merged;                  // the batch's nodes are one axis of the queries' shared tensor map, else sequences are its last
+    FastDiv group, sequence;      // query heads per cache head; nodes per sequence
+    int *before;                  // [batch + 1] cost of the own blocks before sequence b
+    int *error;                   // [grid]
+    float2 *ml;                   // (reference, sum) of every row of every slot
+    float *o;                     // of every tile of a slot [head_dim / 32][rows][32], not divided by the sum; vectors of four swapped (row & 7)
 };
 
 struct AttKernelArgs {
     AttentionArgs a;
     AttPlan p;
 };
+struct AttMaps { CUtensorMap k, v, q, q_shared, out; };
 
 __device__ __forceinline__ int own_end(const CacheArgs &c, int len) {   // keys of a sequence that is there
     const int64_t slots = static_cast<int64_t>(c.table_width) << c.page_shift;
@@ -105,10 +118,10 @@ __device__ __forceinline__ int split_cta(int cost, int all, int grid) {
     return static_cast<int>(static_cast<unsigned long long>(static_cast<unsigned>(cost)) * grid / static_cast<unsigned>(all));
 }
 
-// Consecutive tiles of one block of rows.
+// Consecutive tiles of keys for one block of rows.
 struct AttPiece {
-    bool shared, two;      // two: more than 128 rows
-    int b, head, block, rows, t0, t1, tiles;
+    bool shared, two;      // two: the block has two tiles of rows
+    int b, head, block, t0, t1, tiles;
     int item;              // among the shared or among the own blocks
     int plain, keys;       // keys that every row sees; all keys
     __device__ bool masked(int t) const { return t >= plain / kTile; }
@@ -119,52 +132,45 @@ struct AttStart { int from, to, at; bool shared; int b, head, block; };   // cos
 struct AttWalk {
     const CacheArgs &c;
     const AttPlan &p;
-    int shared_len, from, to, at, b, head, block, len, tiles;
+    int shared_len, from, to, at, b, head, block, len, next_len, tiles;
     bool shared;
 
     __device__ AttWalk(const AttKernelArgs &K, const AttStart &s)
-        : c(K.a.c), p(K.p), shared_len(K.a.shared_len), from(s.from), to(s.to), at(s.at), b(s.b), head(s.head), block(s.block), shared(s.shared) {
-        look();
+        : c(K.a.c), p(K.p), shared_len(K.a.shared_len), from(s.from), to(s.to), at(s.at), b(s.b), head(s.head), block(s.block), len(0), shared(s.shared) {
+        next_len = at < to ? c.lens[b] : -1;
+        if (shared) tiles = p.shared_tiles;
+        else look();
     }
-    __device__ void look() {
-        if (shared) { tiles = p.shared_tiles; return; }
+    __device__ void look() {   // the next sequence that is there
         tiles = 0;
         if (at >= to) return;
         for (; b < c.batch; ++b) {
-            len = c.lens[b];
+            len = next_len;
+            next_len = b + 1 < c.batch ? c.lens[b + 1] : -1;
             tiles = own_tiles(c, len);
             if (tiles) break;
         }
     }
     __device__ bool next(AttPiece &x) {
         while (at < to && tiles) {
+            const AttRows &r = shared ? p.shared : p.own;
             x.shared = shared;
             x.head = head;
             x.block = block;
             x.tiles = tiles;
+            x.two = 2 * block + 1 < r.tiles;
             x.t0 = from > at ? tiles_before(from - at, tiles) : 0;
             x.t1 = tiles_before(to - at, tiles);
-            int rows;
-            if (shared) {
-                x.b = 0;
-                x.item = head * p.shared_blocks + block;
-                x.plain = x.keys = shared_len;
-                rows = c.batch * c.nodes * p.group.d;
-            } else {
-                x.b = b;
-                x.item = (b * c.kv_heads + head) * p.own_blocks + block;
-                x.keys = own_end(c, len);
-                x.plain = min(len, x.keys);
-                rows = c.nodes * p.group.d;
-            }
-            x.rows = min(kBlockRows, rows - block * kBlockRows);
-            x.two = x.rows > kTile;
+            x.b = shared ? 0 : b;
+            x.item = (x.b * c.kv_heads + head) * r.blocks + block;
+            x.keys = shared ? shared_len : own_end(c, len);
+            x.plain = shared ? shared_len : min(len, x.keys);
             at += block_cost(tiles);
-            if (++block == (shared ? p.shared_blocks : p.own_blocks)) {
+            if (++block == r.blocks) {
                 block = 0;
                 if (++head == c.kv_heads) {
                     head = 0;
-                    if (shared) { shared = false; b = 0; }
+                    if (shared) shared = false;   // (b is the first)
                     else ++b;
                     look();
                 }
@@ -175,14 +181,15 @@ struct AttWalk {
     }
 };
 
-// Where row `i` of a block is.
-struct AttRow { int b, n, h; };
-__device__ __forceinline__ AttRow row_of(const AttPlan &p, const AttPiece &x, int i) {
-    const unsigned r = x.block * kBlockRows + i, node = p.group.quot(r);
-    AttRow o;
-    o.h = x.head * p.group.d + (r - node * p.group.d);
-    if (x.shared) { o.b = p.nodes.quot(node); o.n = node - o.b * p.nodes.d; }
-    else { o.b = x.b; o.n = node; }
+// Where a tile of rows begins: node among those of the batch (shared) or of the sequence, and its nodes.
+struct AttTile { int node, count; };
+__device__ __forceinline__ AttTile tile_of(const AttKernelArgs &K, bool shared, int tile) {
+    const CacheArgs &c = K.a.c;
+    const AttRows &r = shared ? K.p.shared : K.p.own;
+    const int period = r.parts == 1 ? tile : r.by_parts.quot(tile), part = tile - period * r.parts;
+    AttTile o;
+    o.node = period * r.period + part * r.nodes;
+    o.count = min(r.nodes, min((period + 1) * r.period, shared ? c.batch * c.nodes : c.nodes) - o.node);
     return o;
 }
 
@@ -212,6 +219,10 @@ template <class T> __device__ __forceinline__ bool not_finite(uint16_t e);
 template <> __device__ __forceinline__ bool not_finite<__nv_bfloat16>(uint16_t e) { return (e & 0x7f80) == 0x7f80; }
 template <> __device__ __forceinline__ bool not_finite<__half>(uint16_t e) { return (e & 0x7c00) == 0x7c00; }
 
+__device__ __forceinline__ void st_shared(uint32_t at, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+
 // 32 columns of a row's output at most: the tree nodes that the row sees and whose value there is no finite number.
 template <class T>
 __device__ __noinline__ void add_not_finite(const AttentionArgs &A, const AttPiece &x, int n, int col0, float *o) {
@@ -229,15 +240,15 @@ __device__ __noinline__ void add_not_finite(const AttentionArgs &A, const AttPie
 }
 
 template <class T, int D>
-__global__ void __launch_bounds__(kAttThreads, 1) attention_kernel(const __grid_constant__ AttKernelArgs K, const __grid_constant__ CUtensorMap map_k,
-                                                                   const __grid_constant__ CUtensorMap map_v) {
+__global__ void __launch_bounds__(kAttThreads, 1) attention_kernel(const __grid_constant__ AttKernelArgs K, const __grid_constant__ AttMaps maps) {
     using L = AttShape<D>;
     constexpr bool kBf16 = Weight<T>::kBf16;
+    constexpr int SK = L::kKeyStages, SV = L::kValueStages;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ __align__(8) uint64_t bars[2 * L::kStages + 11];
+    __shared__ __align__(8) uint64_t bars[2 * (SK + SV) + 13];
     __shared__ uint32_t tmem_base;
     __shared__ int gave_up_, bad_values;
-    __shared__ float2 other[kTile];           // (reference, sum) of the second group's rows
+    __shared__ float2 other[kTile];           // of each row: (reference, sum) of group 1, then both groups' factors
     __shared__ int warp_sum[kAttThreads / 32];
     __shared__ AttStart start;
     volatile int *const gave_up = &gave_up_;
@@ -247,37 +258,43 @@ __global__ void __launch_bounds__(kAttThreads, 1) attention_kernel(const __grid_
     const AttPlan &P = K.p;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     uint8_t *const smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    const uint32_t s_q = saddr(smem), s_kv = s_q + 2 * L::kTileBytes, bar0 = saddr(bars);
-    const auto kv_full = [&](int s) { return bar0 + 8u * s; };
-    const auto kv_empty = [&](int s) { return bar0 + 8u * (L::kStages + s); };
-    const uint32_t bar1 = bar0 + 16u * L::kStages;
+    const uint32_t s_q = saddr(smem), s_k = s_q + 2 * L::kTileBytes, s_v = s_k + SK * L::kTileBytes, bar0 = saddr(bars);
+    const auto k_full = [&](int s) { return bar0 + 8u * s; };
+    const auto k_empty = [&](int s) { return bar0 + 8u * (SK + s); };
+    const auto v_full = [&](int s) { return bar0 + 8u * (2 * SK + s); };
+    const auto v_empty = [&](int s) { return bar0 + 8u * (2 * SK + SV + s); };
+    const uint32_t bar1 = bar0 + 16u * (SK + SV);
     const auto q_full = [&](int q) { return bar1 + 8u * q; };
     const auto q_empty = [&](int q) { return bar1 + 16u + 8u * q; };
     const auto s_full = [&](int t) { return bar1 + 32u + 8u * t; };
     const auto p_full = [&](int t) { return bar1 + 48u + 8u * t; };
     const auto o_full = [&](int t) { return bar1 + 64u + 8u * t; };
-    const uint32_t o_free = bar1 + 80u;
+    const uint32_t o_free = bar1 + 80u, v_here = bar1 + 88u, v_clean = bar1 + 96u;
 
     if (warp == 9) tmem_alloc(saddr(&tmem_base), 512);
     if (tid == 0) {
-        for (int s = 0; s < L::kStages; ++s) { bar_init(kv_full(s), 1); bar_init(kv_empty(s), 1); }
+        for (int s = 0; s < SK; ++s) { bar_init(k_full(s), 1); bar_init(k_empty(s), 1); }
+        for (int s = 0; s < SV; ++s) { bar_init(v_full(s), 1); bar_init(v_empty(s), 1); }
         for (int t = 0; t < 2; ++t) {
-            bar_init(q_full(t), 64); bar_init(q_empty(t), 1);
+            bar_init(q_full(t), 1); bar_init(q_empty(t), 8);
             bar_init(s_full(t), 1); bar_init(p_full(t), kTile); bar_init(o_full(t), 1);
         }
         bar_init(o_free, 2 * kTile);
+        bar_init(v_here, 1);
+        bar_init(v_clean, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         gave_up_ = 0;
         bad_values = 0;
-        tma_prefetch_map(&map_k);
-        tma_prefetch_map(&map_v);
+        tma_prefetch_map(&maps.k);
+        tma_prefetch_map(&maps.v);
+        tma_prefetch_map(&maps.q);
     }
     pdl_begin();
 
     // This CTA's run: own costs of all sequences summed up, in the order of the sequences.
     {
         const int per = (c.batch + kAttThreads - 1) / kAttThreads, b0 = min(c.batch, tid * per), b1 = min(c.batch, b0 + per);
-        const int per_b = c.kv_heads * P.own_blocks;
+        const int per_b = c.kv_heads * P.own.blocks;
         int last = 0, mine = 0;   // of the thread's only or last sequence
         for (int b = b0; b < b1; ++b) {
             last = block_cost(own_tiles(c, c.lens[b]));
@@ -305,7 +322,7 @@ __global__ void __launch_bounds__(kAttThreads, 1) attention_kernel(const __grid_
         if (tid == 0 && from == to) start = AttStart{0, 0, 0, false, 0, 0, 0};
         if (tid == 0 && from < to && from < P.shared_cost) {
             const int each = block_cost(P.shared_tiles), item = from / each;
-            start = AttStart{from, to, item * each, true, 0, item / P.shared_blocks, item % P.shared_blocks};
+            start = AttStart{from, to, item * each, true, 0, item / P.shared.blocks, item % P.shared.blocks};
         }
         if (here && from < to) {
             int b = b0;
@@ -316,7 +333,7 @@ __global__ void __launch_bounds__(kAttThreads, 1) attention_kernel(const __grid_
                     before += last * per_b;
                 }
             const int in_b = (from - before) / last;
-            start = AttStart{from, to, before + in_b * last, false, b, in_b / P.own_blocks, in_b % P.own_blocks};
+            start = AttStart{from, to, before + in_b * last, false, b, in_b / P.own.blocks, in_b % P.own.blocks};
         }
         if (blockIdx.x == 0 && b0 < b1) {   // for the kernel that joins
             before = upto - mine;
@@ -341,14 +358,20 @@ __global__ void __launch_bounds__(kAttThreads, 1) attention_kernel(const __grid_
         const uint32_t lanes = static_cast<uint32_t>(32 * (warp & 3)) << 16;
         const uint32_t t_s = tm + lanes + L::kS + g * kTile, t_p = tm + lanes + L::kP + g * L::kPStep, t_o = tm + lanes + L::kO;
         uint32_t s_phase = 0, o_phase = 0;
+        int q_slot = 0;
         const float cs = A.scale_log2;
-        while (walk.next(x)) {
-            const int row = (x.two ? g * kTile : 0) + gt;
-            const bool warp_on = row - lane < x.rows;   // any row in this warp
-            const AttRow at = row_of(P, x, min(row, x.rows - 1));
+        bool there = walk.next(x);
+        while (there) {
+            const int tile = 2 * x.block + (x.two ? g : 0);
+            const AttTile rows = tile_of(K, x.shared, tile);
+            const int valid = rows.count * P.group.d, in = P.group.quot(gt);   // rows of the tile; the row's node
+            const bool warp_on = gt - lane < valid, mine = gt < valid;           // any row in this warp
             float ref = neg_inf(), sum = 0.f;
             const int step = x.two ? 1 : 2, first = x.two ? x.t0 : x.t0 + g;
             for (int t = first; t < x.t1; t += step) {
+                const bool masked = x.masked(t);
+                uint32_t bits[4] = {};
+                if (masked && warp_on) row_bits(A, x, t, x.shared ? 0 : rows.node + min(in, rows.count - 1), bits);
                 bar_wait(s_full(g), s_phase, gave_up);
                 s_phase ^= 1u;
                 tmem_fence_after();
@@ -357,9 +380,7 @@ __global__ void __launch_bounds__(kAttThreads, 1) attention_kernel(const __grid_
 #pragma unroll
                     for (int i = 0; i < 4; ++i) tmem_ld32_async(t_s + 32 * i, s + 32 * i);
                     tmem_wait_ld(s);
-                    if (x.masked(t)) {
-                        uint32_t bits[4];
-                        row_bits(A, x, t, at.n, bits);
+                    if (masked) {
 #pragma unroll
                         for (int i = 0; i < kTile; ++i) s[i] = bits[i / 32] >> (i & 31) & 1 ? s[i] : neg_inf();
                     }
@@ -373,7 +394,7 @@ __global__ void __launch_bounds__(kAttThreads, 1) attention_kernel(const __grid_
                     }
                     const float top = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3)) * cs - Weight<T>::kBias;
                     if (t == first) ref = top;
-                    else if (__any_sync(kFull, top > ref + kSlack && row < x.rows)) {
+                    else if (__any_sync(kFull, top > ref + kSlack && mine)) {
                         // (the product that added the last tile to O is done: it was issued before these scores)
                         const float now = fmaxf(ref, top), f = now == neg_inf() ? 1.f : ex2(ref - now);
                         sum *= f;
@@ -412,281 +433,306 @@ __global__ void __launch_bounds__(kAttThreads, 1) attention_kernel(const __grid_
                 bar_arrive(p_full(g));
             }
             // ---- the end of the piece ------------------------------------------------------------------
-            const bool any = first < x.t1;
-            if (any) {
+            AttPiece y = {};
+            there = walk.next(y);   // (while the last product runs)
+            if (first < x.t1) {
                 bar_wait(o_full(g), o_phase, gave_up);
                 o_phase ^= 1u;
             }
-            tmem_fence_after();
-            float f0 = 1.f, f1 = 0.f;   // factors of this group's O, of the other group's
-            bool write = warp_on;
-            if (!x.two) {
+            const bool whole = !x.shared && P.shared_tiles == 0 && x.t1 - x.t0 == x.tiles;
+            const bool join = !x.two && x.t1 - x.t0 > 1;   // of both groups
+            float f0 = 1.f, f1 = 0.f;                      // factors of O: of group 0 (a group's own where it is alone), of group 1
+            if (!x.two) {   // the groups have the same rows, and each writes half of the columns
                 if (g == 1) other[gt] = make_float2(ref, sum);
                 tmem_fence_before();
                 asm volatile("bar.sync 1, 256;" ::: "memory");
-                tmem_fence_after();
-                write = warp_on && g == 0;
-                if (g == 0 && x.t1 - x.t0 > 1) {
+                if (g == 0 && join) {
                     const float2 z = other[gt];
-                    const float now = fmaxf(ref, z.x), r = now == neg_inf() ? 0.f : now;
+                    const float both = fmaxf(ref, z.x), r = both == neg_inf() ? 0.f : both;
                     f0 = ex2(ref - r); f1 = ex2(z.x - r);
                     sum = sum * f0 + z.y * f1;
-                    ref = now;
+                    ref = both;
                 }
             }
-            if (write) {
-                const bool whole = !x.shared && P.shared_tiles == 0 && x.t1 - x.t0 == x.tiles, join = !x.two && x.t1 - x.t0 > 1;
-                const bool mine = row < x.rows, none = sum == 0.f;
+            const bool none = sum == 0.f;
+            if (whole) {
                 const float inv = none ? 0.f : 1.f / sum;
+                f0 *= inv; f1 *= inv;
+            }
+            if (!x.two) {
+                if (g == 0) other[gt] = make_float2(f0, f1);
+                asm volatile("bar.sync 1, 256;" ::: "memory");
+                if (g == 1) { const float2 z = other[gt]; f0 = z.x; f1 = z.y; }
+            }
+            tmem_fence_after();
+            const int slot0 = q_slot, slot1 = q_slot ^ 1;   // of queries
+            const uint32_t o0 = t_o + (x.two ? g * D : 0);
+            const int col0 = x.two ? 0 : g * (D / 2), col1 = x.two ? D : col0 + D / 2;
+            const int row_in = 32 * (warp & 3) + lane;
+            if (warp_on) {
                 const int bad = *static_cast<volatile int *>(&bad_values);
-                int64_t slot_row = 0;
+                const AttRows &r = x.shared ? P.shared : P.own;
+                int64_t slot_tile = 0;   // tile of rows in the workspace, counted in such tiles
                 if (!whole) {
-                    slot_row = x.shared ? (x.item + int64_t(blockIdx.x)) * P.shared_rows + row
-                                        : P.slots * P.shared_rows + (x.item + int64_t(blockIdx.x)) * P.own_rows + row;
-                    if (mine) P.ml[slot_row] = make_float2(ref, sum);
-                } else if (mine && A.lse) {
-                    A.lse[(static_cast<int64_t>(at.b) * c.nodes + at.n) * c.heads + at.h] = none ? neg_inf() : (ref + log2f(sum)) * 0.6931471805599453f;
+                    slot_tile = (x.item + int64_t(blockIdx.x)) * r.slot_tiles + (x.two ? g : 0);
+                    const int64_t row0 = x.shared ? slot_tile * r.slot_rows : P.shared_slots * P.shared.slot_tiles * P.shared.slot_rows + slot_tile * r.slot_rows;
+                    slot_tile = row0;
+                    if (mine && (x.two || g == 0)) P.ml[row0 + gt] = make_float2(ref, sum);
+                } else if (mine && A.lse && (x.two || g == 0)) {
+                    A.lse[(static_cast<int64_t>(x.b) * c.nodes + rows.node + in) * c.heads + x.head * P.group.d + (gt - in * P.group.d)] =
+                        none ? neg_inf() : (ref + log2f(sum)) * 0.6931471805599453f;
                 }
+                // 4 KB (two of them for a group that is alone in 32) of this warp
+                const uint32_t tile_at = D == 64 ? s_v + SV * L::kTileBytes + (x.two ? g : 0) * L::kTileBytes : s_q + (x.two && g ? slot1 : slot0) * L::kTileBytes;
+                const uint32_t own_at = D == 64 ? s_v + SV * L::kTileBytes + 4096 * warp
+                                                : tile_at + (x.two ? 8192 * (warp & 3) : 4096 * warp);
+                const uint32_t lane_rows = min(32, valid - (gt - lane));
 #pragma unroll 1
-                for (int i = 0; i < D; i += 32) {
+                for (int i = col0; i < col1; i += 32) {
                     float o[32];
-                    tmem_ld32(t_o + g * D + i, o);
+                    tmem_ld32(o0 + i, o);
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) o[j] *= f0;
                     if (join) {
                         float z[32];
                         tmem_ld32(t_o + D + i, z);
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) o[j] = o[j] * f0 + z[j] * f1;
+                        for (int j = 0; j < 32; ++j) o[j] = fmaf(z[j], f1, o[j]);
                     }
                     if (bad && !x.shared && mine) {
                         float z[32];
 #pragma unroll
                         for (int j = 0; j < 32; ++j) z[j] = o[j];
-                        add_not_finite<T>(A, x, at.n, i, z);
+                        add_not_finite<T>(A, x, rows.node + in, i, z);
 #pragma unroll
                         for (int j = 0; j < 32; ++j) o[j] = z[j];
                     }
-                    if (mine && whole) {
-                        T *dst = static_cast<T *>(A.out.data) + at.b * A.out.seq + at.n * A.out.node + at.h * A.out.head + i;
-#pragma unroll
-                        for (int j = 0; j < 32; j += 8) {
-                            uint4 u;
-                            u.x = pack2<T>(o[j] * inv, o[j + 1] * inv); u.y = pack2<T>(o[j + 2] * inv, o[j + 3] * inv);
-                            u.z = pack2<T>(o[j + 4] * inv, o[j + 5] * inv); u.w = pack2<T>(o[j + 6] * inv, o[j + 7] * inv);
-                            *reinterpret_cast<uint4 *>(dst + j) = u;
-                        }
-                    } else if (mine) {
-                        float *dst = P.o + slot_row * D + i;
-#pragma unroll
-                        for (int j = 0; j < 32; j += 4) *reinterpret_cast<float4 *>(dst + j) = make_float4(o[j], o[j + 1], o[j + 2], o[j + 3]);
-                    }
                     __syncwarp();
+                    if (whole) {
+                        const uint32_t at = tile_at + (i / 64) * L::kHalfBytes + row_in * 128;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const float *y8 = o + 8 * j;
+                            st_shared(at + (((i & 32) / 8 + j) ^ (row_in & 7)) * 16, pack2<T>(y8[0], y8[1]), pack2<T>(y8[2], y8[3]),
+                                      pack2<T>(y8[4], y8[5]), pack2<T>(y8[6], y8[7]));
+                        }
+                    } else {
+                        const uint32_t at = own_at + (D == 128 && x.two ? (i & 32) * 128 : 0);
+                        if (lane == 0 && (D == 64 || !x.two || (i & 32) == 0)) store_wait_read();
+                        __syncwarp();
+#pragma unroll
+                        for (int j = 0; j < 8; ++j)
+                            st_shared(at + lane * 128 + (j ^ (lane & 7)) * 16, __float_as_uint(o[4 * j]), __float_as_uint(o[4 * j + 1]), __float_as_uint(o[4 * j + 2]),
+                                      __float_as_uint(o[4 * j + 3]));
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                        __syncwarp();
+                        if (lane == 0) {
+                            bulk_store(P.o + slot_tile * D + (i / 32) * int64_t(r.slot_rows) * 32 + (gt - lane) * 32, at, lane_rows * 128);
+                            store_commit();
+                        }
+                    }
                 }
             }
             tmem_fence_before();
             bar_arrive(o_free);
+            if (whole) {
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                if (x.two && g == 0) asm volatile("bar.sync 2, 128;" ::: "memory");
+                else if (x.two) asm volatile("bar.sync 3, 128;" ::: "memory");
+                else asm volatile("bar.sync 1, 256;" ::: "memory");
+                if (lane == 0 && (x.two ? (warp & 3) == 0 : warp == 0)) {
+                    const uint32_t at = D == 64 ? s_v + SV * L::kTileBytes + (x.two ? g : 0) * L::kTileBytes : s_q + (x.two && g ? slot1 : slot0) * L::kTileBytes;
+                    for (int h = 0; h < L::kHalves; ++h) tma_store(&maps.out, at + h * L::kHalfBytes, 64 * h, x.head * P.group.d, rows.node, x.b);
+                    store_commit();
+                }
+            }
+            // the queries' slots may be filled again
+            if (lane == 0) {
+                store_wait_read();
+                if (x.two) bar_arrive(q_empty(g ? slot1 : slot0), 2);
+                else bar_arrive(q_empty(slot0), 1);
+            }
+            __syncwarp();
+            if (!x.two) q_slot ^= 1;
+            x = y;
         }
-    } else if (fewer_registers<kOtherRegs>(), warp == 8) {
-        // ---- K and V tiles -------------------------------------------------------------------------
-        int stage = 0;
-        uint32_t phase = 0;
+        if (lane == 0) store_wait();
+    } else if (fewer_registers<kOtherRegs>(), warp == 8 || warp == 11) {
+        // ---- tiles of keys (warp 8, and queries) and values (warp 11) -------------------------------------------
+        const bool keys = warp == 8;
+        const int stages = keys ? SK : SV;
+        const uint32_t ring = keys ? s_k : s_v, full = keys ? k_full(0) : v_full(0), empty = keys ? k_empty(0) : v_empty(0);
+        const CUtensorMap *const map = keys ? &maps.k : &maps.v;
+        int stage = 0, q_slot = 0;
+        uint32_t phase = 1, q_phase = 1;
         const int ps = 1 << c.page_shift, box = min(ps, kTile), boxes = kTile / box;
         const auto page_at = [&](int t) -> int {   // lane i: the page of the tile's i-th box (c.pages: reads as zeros)
-            const int64_t slot = t * int64_t(kTile) + lane * box;
+            const int slot = t * kTile + lane * box;
             if (lane >= boxes || t >= x.t1 || slot >= x.keys) return c.pages;
-            int page;
-            if (x.shared) page = A.shared_table[slot >> c.page_shift];
-            else {
-                const int64_t at = slot >> c.page_shift;
-                if (at >= c.table_width) return c.pages;
-                page = c.table[x.b * c.stride_table + at];
-            }
+            const int at = slot >> c.page_shift;
+            const int page = x.shared ? A.shared_table[at] : c.table[x.b * c.stride_table + at];   // (no key lies behind the table)
             return page >= 0 && page < c.pages ? page : c.pages;
         };
-        const auto bring = [&](const CUtensorMap *map, int t, int page) {
-            bar_wait(kv_empty(stage), phase ^ 1u, gave_up);
-            if (lane == 0) bar_expect(kv_full(stage), L::kTileBytes);
-            __syncwarp();
-            if (lane < boxes) {
-                const uint32_t dst = s_kv + stage * L::kTileBytes + lane * box * 128;
-                const int y = ps > kTile ? static_cast<int>((t * int64_t(kTile)) & (ps - 1)) : 0;
-#pragma unroll
-                for (int h = 0; h < L::kHalves; ++h) tma_load(dst + h * L::kHalfBytes, map, 64 * h, y, x.head, page, kv_full(stage));
-            }
-            if (++stage == L::kStages) { stage = 0; phase ^= 1u; }
-        };
         while (walk.next(x)) {
-            const int ahead = x.two ? 1 : 2;   // keys are this many tiles ahead of the values
-            int p0 = page_at(x.t0), p1 = page_at(x.t0 + 1), p2 = page_at(x.t0 + 2);
-            bring(&map_k, x.t0, p0);
-            if (ahead == 2 && x.t0 + 1 < x.t1) bring(&map_k, x.t0 + 1, p1);
+            int page = page_at(x.t0);
             for (int t = x.t0; t < x.t1; ++t) {
-                const int p3 = page_at(t + 3);
-                bring(&map_v, t, p0);
-                if (t + ahead < x.t1) bring(&map_k, t + ahead, ahead == 1 ? p1 : p2);
-                p0 = p1; p1 = p2; p2 = p3;
+                const int next = page_at(t + 1);
+                bar_wait(empty + 8 * stage, phase, gave_up);
+                if (lane == 0) bar_expect(full + 8 * stage, L::kTileBytes);
+                __syncwarp();
+                if (lane < boxes) {
+                    const uint32_t dst = ring + stage * L::kTileBytes + lane * box * 128;
+                    const int y = ps > kTile ? (t * kTile) & (ps - 1) : 0;
+#pragma unroll
+                    for (int h = 0; h < L::kHalves; ++h) tma_load(dst + h * L::kHalfBytes, map, 64 * h, y, x.head, page, full + 8 * stage);
+                }
+                __syncwarp();
+                if (++stage == stages) { stage = 0; phase ^= 1u; }
+                page = next;
+                if (keys && t == x.t0) {   // (behind the first keys: a slot may not be free yet)
+                    const AttRows &r = x.shared ? P.shared : P.own;
+                    for (int i = 0; i < (x.two ? 2 : 1); ++i) {
+                        bar_wait(q_empty(q_slot), q_phase, gave_up);
+                        if (lane == 0) {
+                            const AttTile o = tile_of(K, x.shared, 2 * x.block + i);
+                            int z = o.node, w = x.b;
+                            if (x.shared) {
+                                w = P.merged ? 0 : P.sequence.quot(o.node);
+                                z = o.node - w * c.nodes;
+                            }
+                            bar_expect(q_full(q_slot), r.nodes * P.group.d * 2 * D);   // (what is out of range counts too)
+                            for (int h = 0; h < L::kHalves; ++h)
+                                tma_load(s_q + q_slot * L::kTileBytes + h * L::kHalfBytes, x.shared ? &maps.q_shared : &maps.q, 64 * h, x.head * P.group.d, z, w,
+                                         q_full(q_slot));
+                        }
+                        __syncwarp();
+                        if (++q_slot == 2) { q_slot = 0; q_phase ^= 1u; }
+                    }
+                }
             }
         }
-        // the ring's last arrivals come before the CTA ends
-        for (int s = 0; s < L::kStages; ++s) {
-            bar_wait(kv_empty(stage), phase ^ 1u, gave_up);
-            if (++stage == L::kStages) { stage = 0; phase ^= 1u; }
+        // the rings' last arrivals come before the CTA ends
+        for (int s = 0; s < stages; ++s) {
+            bar_wait(empty + 8 * stage, phase, gave_up);
+            if (++stage == stages) { stage = 0; phase ^= 1u; }
+        }
+        for (int s = 0; s < 2 && keys; ++s) {
+            bar_wait(q_empty(q_slot), q_phase, gave_up);
+            if (++q_slot == 2) { q_slot = 0; q_phase ^= 1u; }
         }
     } else if (warp == 9) {
-        // ---- matrix instructions -------------------------------------------------------------------
-        int stage = 0;
-        uint32_t phase = 0, q_phase = 0, p_phase = 0, free_phase = 1;
-        int q_slot = 0;
-        constexpr uint32_t desc_s = mma_desc(kBf16, kTile, false), desc_o = mma_desc(kBf16, D, true);
-        const auto arrived = [&]() {   // the next stage of the ring
-            bar_wait(kv_full(stage), phase, gave_up);
-            const int s = stage;
-            if (++stage == L::kStages) { stage = 0; phase ^= 1u; }
-            return s;
-        };
-        const bool lead = lane == 0;
-        const uint32_t tmu = uniform(tm), kv_op = operand(uniform(s_kv), L::kHalfBytes), q_op = operand(uniform(s_q), L::kHalfBytes);
-        const auto scores = [&](int t, int q, int s) {   // S_t = Q_q K^T
-            uint32_t a = uniform(q_op + q * (L::kTileBytes >> 4)), b = uniform(kv_op + s * (L::kTileBytes >> 4));
-            const uint32_t d = uniform(tmu + L::kS + t * kTile);
-#pragma unroll 1
-            for (int h = 0; h < L::kHalves; ++h) {
-#pragma unroll
-                for (int k = 0; k < 4; ++k) mma_ss(d, a + 2 * k, b + 2 * k, desc_s, h + k > 0, lead);
-                a += L::kHalfBytes >> 4;
-                b += L::kHalfBytes >> 4;
-            }
-            mma_commit(s_full(t), lead);
-        };
-        const auto products = [&](int t, int s, bool add) {   // O_t (+)= P_t V
-            uint32_t a = uniform(tmu + L::kP + t * L::kPStep), b = uniform(kv_op + s * (L::kTileBytes >> 4));
-            const uint32_t d = uniform(tmu + L::kO + t * D);
-            bar_wait(p_full(t), p_phase >> t & 1u, gave_up);
-            p_phase ^= 1u << t;
-            tmem_fence_after();
-#pragma unroll 1
-            for (int h = 0; h < 2; ++h) {
-#pragma unroll
-                for (int k = 0; k < 4; ++k) mma_ts(d, a + 8 * k, b + k * (2048 >> 4), desc_o, add || h + k > 0, lead);
-                a += 32;
-                b += 4 * (2048 >> 4);
-            }
-        };
-        // values behind the end, and those of tree nodes that are no numbers: zero
-        const auto clear = [&](int tile, int s) {
-            constexpr int kVecs = D / 8;
-            constexpr uint32_t kExp = kBf16 ? 0x7f807f80u : 0x7c007c00u;   // all ones: no finite number
-            const int r0 = max(0, x.plain - tile * kTile), r1 = min(kTile, x.keys - tile * kTile);
-            uint8_t *const v = smem + 2 * L::kTileBytes + s * L::kTileBytes;
-            const auto at = [&](int i) { return reinterpret_cast<uint4 *>(v + (i % kVecs / 8) * L::kHalfBytes + (i / kVecs) * 128 + (i % 8) * 16); };
-            bool bad = false;
-            for (int i = lane + r0 * kVecs; i < r1 * kVecs; i += 128) {
-                uint4 u[4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) u[j] = i + 32 * j < r1 * kVecs ? *at(i + 32 * j) : make_uint4(0, 0, 0, 0);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    uint32_t *w = &u[j].x, hit = 0;
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const uint32_t t = (w[k] & kExp) ^ kExp;   // a half that is zero: no finite number
-                        hit |= (t - 0x00010001u) & ~t & 0x80008000u;
+        // ---- matrix instructions: one thread ---------------------------------------------------------
+        if (lane == 0) {
+            int ks = 0, vs = 0, q_slot = 0;
+            uint32_t k_phase = 0, v_phase = 0, q_phase = 0, p_phase = 0, free_phase = 1, clean_phase = 0;
+            constexpr uint32_t desc_s = mma_desc(kBf16, kTile, false), desc_o = mma_desc(kBf16, D, true);
+            const uint32_t k_op = operand(s_k, L::kHalfBytes), v_op = operand(s_v, L::kHalfBytes), q_op = operand(s_q, L::kHalfBytes);
+            const auto queries = [&]() {
+                bar_wait_one(q_full(q_slot), q_phase, gave_up);
+                const int s = q_slot;
+                if (++q_slot == 2) { q_slot = 0; q_phase ^= 1u; }
+                return s;
+            };
+            bool there = walk.next(x);
+            while (there) {
+                AttPiece y = {};
+                bool then = false;
+                // queries of both groups, or of one tile in whichever slot is next
+                const int q0 = queries(), q1 = x.two ? queries() : q0, ahead = x.two ? 1 : 2;
+                // Products of tile t, scores of tile t + ahead: each once in the code, which other warps push out of the instruction cache.
+                for (int t = x.t0 - ahead; t < x.t1; ++t) {
+                    const bool now = t >= x.t0, more = t + ahead < x.t1;
+                    if (now) {
+                        bar_wait_one(v_full(vs), v_phase, gave_up);
+                        if (x.masked(t)) {
+                            bar_arrive(v_here);
+                            if (t == x.t1 - 1) then = walk.next(y);   // (meanwhile)
+                            bar_wait_one(v_clean, clean_phase, gave_up);
+                            clean_phase ^= 1u;
+                        } else if (t == x.t1 - 1) then = walk.next(y);
+                        if (t == x.t0) {   // O of the piece before has been read by now or soon
+                            bar_wait_one(o_free, free_phase, gave_up);
+                            free_phase ^= 1u;
+                        }
                     }
-                    if (hit) {
-                        bad = true;
+                    if (more && (x.two || !now)) bar_wait_one(k_full(ks), k_phase, gave_up);
+                    const int g0 = x.two ? 0 : (t + ahead - x.t0) & 1, g1 = x.two ? 2 : g0 + 1;
+                    for (int g = g0; g < g1; ++g) {
+                        if (now) {   // O_g (+)= P_g V
+                            const uint32_t a = tm + L::kP + g * L::kPStep, b = v_op + vs * (L::kTileBytes >> 4), d = tm + L::kO + g * D;
+                            const bool add = t >= x.t0 + ahead;
+                            bar_wait_one(p_full(g), p_phase >> g & 1u, gave_up);
+                            p_phase ^= 1u << g;
+                            tmem_fence_after();
+#pragma unroll
+                            for (int k = 0; k < kTile / 16; ++k) mma_ts(d, a + 8 * k, b + k * (2048 >> 4), desc_o, add || k > 0);
+                            if (g == g1 - 1) mma_commit(v_empty(vs));
+                        }
+                        if (more) {   // S_g = Q K^T
+                            if (now && !x.two) bar_wait_one(k_full(ks), k_phase, gave_up);   // (the products first: these keys may still be on their way)
+                            const uint32_t a = q_op + (g ? q1 : q0) * (L::kTileBytes >> 4), b = k_op + ks * (L::kTileBytes >> 4), d = tm + L::kS + g * kTile;
+#pragma unroll
+                            for (int k = 0; k < D / 16; ++k) {
+                                const uint32_t off = ((k / 4) * L::kHalfBytes + (k % 4) * 32) >> 4;
+                                mma_ss(d, a + off, b + off, desc_s, k > 0);
+                            }
+                            mma_commit(s_full(g));
+                            if (g == g1 - 1) mma_commit(k_empty(ks));
+                        } else if (now) mma_commit(o_full(g));
+                    }
+                    if (now && ++vs == SV) { vs = 0; v_phase ^= 1u; }
+                    if (more && ++ks == SK) { ks = 0; k_phase ^= 1u; }
+                }
+                x = y;
+                there = then;
+            }
+            bar_wait_one(o_free, free_phase, gave_up);
+        }
+        __syncwarp();
+    } else {
+        // ---- values behind the end, and those of tree nodes that are no numbers: zero -----------------------
+        int n0 = 0;   // tile among the CTA's, of the piece's first
+        uint32_t here_phase = 0;
+        for (; walk.next(x); n0 += x.t1 - x.t0) {
+            for (int t = max(x.t0, x.plain / kTile); t < x.t1; ++t) {
+                const unsigned n = n0 + t - x.t0, s = n % SV;
+                bar_wait(v_here, here_phase, gave_up);   // (asked for: the ring is neither before nor behind this place)
+                here_phase ^= 1u;
+                bar_wait(v_full(s), (n / SV) & 1u, gave_up);
+                constexpr int kVecs = D / 8;
+                constexpr uint32_t kExp = kBf16 ? 0x7f807f80u : 0x7c007c00u;   // all ones: no finite number
+                const int r0 = max(0, x.plain - t * kTile), r1 = min(kTile, x.keys - t * kTile);
+                uint8_t *const v = smem + (2 + SK + s) * L::kTileBytes;
+                const auto place = [&](int i) { return reinterpret_cast<uint4 *>(v + (i % kVecs / 8) * L::kHalfBytes + (i / kVecs) * 128 + (i % 8) * 16); };
+                for (int i = lane + r1 * kVecs; i < kTile * kVecs; i += 32) *place(i) = make_uint4(0, 0, 0, 0);
+                uint32_t most = 0;   // of the magnitudes, as numbers of 15 bits
+                for (int i0 = r0 * kVecs; i0 < r1 * kVecs; i0 += 256) {
+                    uint4 u[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) u[j] = *place(min(i0 + 32 * j + lane, r1 * kVecs - 1));
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        most = __vimax3_u16x2(most, u[j].x & 0x7fff7fffu, u[j].y & 0x7fff7fffu);
+                        most = __vimax3_u16x2(most, u[j].z & 0x7fff7fffu, u[j].w & 0x7fff7fffu);
+                    }
+                }
+                if (__any_sync(kFull, (most & 0xffffu) >= (kExp & 0xffffu) || most >> 16 >= kExp >> 16)) {
+                    for (int i = lane + r0 * kVecs; i < r1 * kVecs; i += 32) {
+                        uint4 u = *place(i);
+                        uint32_t *w = &u.x;
                         for (int k = 0; k < 4; ++k) {
                             if ((w[k] & kExp & 0xffffu) == (kExp & 0xffffu)) w[k] &= 0xffff0000u;
                             if ((w[k] & kExp & 0xffff0000u) == (kExp & 0xffff0000u)) w[k] &= 0xffffu;
                         }
-                        *at(i + 32 * j) = u[j];
+                        *place(i) = u;
                     }
-                }
-            }
-            for (int i = lane + r1 * kVecs; i < kTile * kVecs; i += 32) *at(i) = make_uint4(0, 0, 0, 0);
-            if (__any_sync(kFull, bad) && lane == 0) *static_cast<volatile int *>(&bad_values) = 1;
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            __threadfence_block();
-            __syncwarp();
-        };
-        while (walk.next(x)) {
-            // Queries of both groups, or of one block in whichever slot is next.
-            int q0 = q_slot, q1;
-            bar_wait(q_full(q_slot), q_phase, gave_up);
-            if (++q_slot == 2) { q_slot = 0; q_phase ^= 1u; }
-            q1 = x.two ? q_slot : q0;
-            if (x.two) {
-                bar_wait(q_full(q_slot), q_phase, gave_up);
-                if (++q_slot == 2) { q_slot = 0; q_phase ^= 1u; }
-            }
-            // Products of tile t, scores of tile t + ahead: each once in the code, which other warps push out of the instruction cache.
-            const int ahead = x.two ? 1 : 2;
-            for (int t = x.t0 - ahead; t < x.t1; ++t) {
-                const bool now = t >= x.t0, more = t + ahead < x.t1;
-                int v = 0, s = 0;
-                if (t == x.t0) {   // O of the piece before has been read by now or soon, and what was said of its values
-                    bar_wait(o_free, free_phase, gave_up);
-                    free_phase ^= 1u;
-                    tmem_fence_after();
-                    if (lane == 0) *static_cast<volatile int *>(&bad_values) = 0;
-                    __syncwarp();
-                }
-                if (now) {
-                    v = arrived();
-                    if (x.masked(t)) clear(t, v);
-                }
-                const int g0 = x.two ? 0 : (t + ahead - x.t0) & 1, g1 = x.two ? 2 : g0 + 1;
-                for (int g = g0; g < g1; ++g) {
-                    if (now) {
-                        products(g, v, t >= x.t0 + ahead);
-                        if (g == g1 - 1) mma_commit(kv_empty(v), lead);
-                    }
-                    if (more) {
-                        if (g == g0) s = arrived();
-                        scores(g, g ? q1 : q0, s);
-                        if (g == g1 - 1) {
-                            mma_commit(kv_empty(s), lead);
-                            if (t + ahead == x.t1 - 1) {   // the last ones
-                                mma_commit(q_empty(q0), lead);
-                                if (x.two) mma_commit(q_empty(q1), lead);
-                            }
-                        }
-                    } else if (now) mma_commit(o_full(g), lead);
-                }
-            }
-        }
-        // (the last arrivals come before the CTA ends)
-        bar_wait(o_free, free_phase, gave_up);
-    } else if (warp >= 10) {
-        // ---- queries -----------------------------------------------------------------------------------
-        constexpr int kVecs = D / 8, kStep = 64 / kVecs, kBatch = 8;   // rows that the two warps bring at once; loads in flight per thread
-        int slot = 0;
-        uint32_t phase = 1;
-        const int qt = tid - 320, vec = qt % kVecs;
-        while (walk.next(x)) {
-            for (int i = 0; i < (x.two ? 2 : 1); ++i) {
-                bar_wait(q_empty(slot), phase, gave_up);
-                uint8_t *dst = smem + slot * L::kTileBytes + (vec / 8) * L::kHalfBytes;
-                const int rows = min(kTile, x.rows - i * kTile);   // (what the other rows hold matters to nobody)
-                for (int r0 = qt / kVecs; r0 < rows; r0 += kBatch * kStep) {
-                    uint4 u[kBatch];
-#pragma unroll
-                    for (int j = 0; j < kBatch; ++j) {
-                        const AttRow o = row_of(P, x, i * kTile + min(rows - 1, r0 + j * kStep));
-                        u[j] = *reinterpret_cast<const uint4 *>(static_cast<const T *>(A.q.data) + o.b * A.q.seq + o.n * A.q.node + o.h * A.q.head + vec * 8);
-                    }
-#pragma unroll
-                    for (int j = 0; j < kBatch; ++j) {
-                        const int r = r0 + j * kStep;
-                        if (r < rows) *reinterpret_cast<uint4 *>(dst + r * 128 + ((vec & 7) ^ (r & 7)) * 16) = u[j];
-                    }
+                    *static_cast<volatile int *>(&bad_values) = 1;   // (from here on the CTA looks for such nodes)
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                bar_arrive(q_full(slot));
-                if (++slot == 2) { slot = 0; phase ^= 1u; }
+                __threadfence_block();
+                __syncwarp();
+                if (lane == 0) bar_arrive(v_clean);
             }
-        }
-        for (int i = 0; i < 2; ++i) {
-            bar_wait(q_empty(slot), phase, gave_up);
-            if (++slot == 2) { slot = 0; phase ^= 1u; }
         }
     }
     tmem_fence_before();
@@ -702,7 +748,7 @@ __global__ void __launch_bounds__(kAttThreads, 1) attention_kernel(const __grid_
 
 constexpr int kJoinThreads = 256, kJoinRows = 32;
 
-// Joins the pieces of every block that has more than one, kJoinRows of its rows per CTA, a warp per row; and finds bad pages (the first
+// Joins the pieces of every block that has more than one, kJoinRows rows of a tile per CTA, a warp per row; and finds bad pages (the first
 // `batch` CTAs, if wanted).
 template <class T, int D>
 __global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(const __grid_constant__ AttKernelArgs K) {
@@ -733,28 +779,36 @@ __global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(const __gr
         }
         block -= c.batch;
     }
-    const int chunks = (P.own_rows + kJoinRows - 1) / kJoinRows, chunk = block % chunks;
-    const int item = block / chunks, per_b = c.kv_heads * P.own_blocks, b = item / per_b, in_b = item - b * per_b;
+    const int chunks = (P.own.slot_rows + kJoinRows - 1) / kJoinRows, chunk = block % chunks;   // of a tile of rows
+    block /= chunks;
+    const int tb = block % P.own.slot_tiles, item = block / P.own.slot_tiles, per_b = c.kv_heads * P.own.blocks, b = item / per_b, in_b = item - b * per_b;
     const int len = c.lens[b];
     if (len < 0) return;
     const int tiles = own_tiles(c, len), each = block_cost(tiles), all = P.before[c.batch];
-    const int own0 = P.before[b] + in_b * each;                       // the block's cost interval, and where its tiles begin
+    const int own0 = P.before[b] + in_b * each;                       // the block's costs begin here, its tiles' kBlockCost later
     const int c0 = split_cta(own0 + kBlockCost, all, P.grid), c1 = split_cta(own0 + each - 1, all, P.grid);
     if (P.shared_tiles == 0 && tiles_before(split_first(c0 + 1, all, P.grid) - own0, tiles) == tiles) return;   // finished in place
-    const int hk = in_b / P.own_blocks, first = (in_b - hk * P.own_blocks) * kBlockRows, rows = min(P.own_rows, c.nodes * static_cast<int>(P.group.d) - first);
+    const int hk = in_b / P.own.blocks, tile = 2 * (in_b - hk * P.own.blocks) + tb;
+    if (tile >= P.own.tiles) return;
+    const AttTile t = tile_of(K, false, tile);
+    const int rows = t.count * P.group.d;
     for (int row = chunk * kJoinRows + (tid >> 5); row < min(rows, (chunk + 1) * kJoinRows); row += kJoinThreads / 32) {
+        const int in = P.group.quot(row), n = t.node + in, h = hk * P.group.d + (row - in * P.group.d);
         float ref = neg_inf(), sum = 0.f, o[E] = {};
-        // pieces of CTAs i0..i1 of a block at `at` in the costs (one whose run has no tile of it left nothing)
-        const auto add = [&](int at, int n, int i0, int i1, int64_t slot_row, int step) {
+        // the pieces of CTAs i0..i1 of a block whose costs begin at `at` (one whose run has no tile of it left nothing); `row0`: the first
+        // row of CTA 0's tile, `step`: rows from one CTA's to the next one's
+        const auto add = [&](int at, int n_tiles, int i0, int i1, int64_t row0, int step, int rows_of, int r) {
             for (int i = i0; i <= i1; ++i) {
-                const int t0 = tiles_before(split_first(i, all, P.grid) - at, n), t1 = tiles_before(split_first(i + 1, all, P.grid) - at, n);
+                const int t0 = tiles_before(split_first(i, all, P.grid) - at, n_tiles), t1 = tiles_before(split_first(i + 1, all, P.grid) - at, n_tiles);
                 if (t1 <= t0) continue;
-                const float2 ml = P.ml[slot_row + int64_t(i) * step];
-                const float *src = P.o + (slot_row + int64_t(i) * step) * D + lane * E;
+                const int64_t first = row0 + int64_t(i) * step;
+                const float2 ml = P.ml[first + r];
+                const int col = lane * E;
+                const float *src = P.o + first * D + (int64_t(col / 32) * rows_of + r) * 32 + ((col % 32 / 4) ^ (r & 7)) * 4 + col % 4;
                 float z[E];
                 if (E == 4) { const float4 v = *reinterpret_cast<const float4 *>(src); z[0] = v.x; z[1] = v.y; z[E - 2] = v.z; z[E - 1] = v.w; }
                 else { const float2 v = *reinterpret_cast<const float2 *>(src); z[0] = v.x; z[1] = v.y; }
-                const float now = fmaxf(ref, ml.x), r = now == neg_inf() ? 0.f : now, f0 = ex2(ref - r), f1 = ex2(ml.x - r);
+                const float now = fmaxf(ref, ml.x), m = now == neg_inf() ? 0.f : now, f0 = ex2(ref - m), f1 = ex2(ml.x - m);
                 sum = sum * f0 + ml.y * f1;
                 ref = now;
 #pragma unroll
@@ -762,15 +816,17 @@ __global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(const __gr
             }
         };
         if (P.shared_tiles) {
-            const int64_t r = static_cast<int64_t>(b) * c.nodes * P.group.d + first + row;
-            const int in = hk * P.shared_blocks + static_cast<int>(r / kBlockRows), s_each = block_cost(P.shared_tiles), at = in * s_each;
+            const AttRows &r = P.shared;
+            const int node = b * c.nodes + n, period = r.by_period.quot(node), in_p = node - period * r.period, part = r.by_nodes.quot(in_p);
+            const int s_tile = period * r.parts + part, s_row = (in_p - part * r.nodes) * P.group.d + (row - in * P.group.d);
+            const int s_item = hk * r.blocks + s_tile / 2, s_each = block_cost(P.shared_tiles), at = s_item * s_each, step = r.slot_tiles * r.slot_rows;
             add(at, P.shared_tiles, split_cta(at + kBlockCost, all, P.grid), split_cta(at + s_each - 1, all, P.grid),
-                int64_t(in) * P.shared_rows + r % kBlockRows, P.shared_rows);
+                int64_t(s_item) * step + s_tile % 2 * r.slot_rows, step, r.slot_rows, s_row);
         }
-        add(own0, tiles, c0, c1, P.slots * P.shared_rows + int64_t(item) * P.own_rows + row, P.own_rows);
+        const int step = P.own.slot_tiles * P.own.slot_rows;
+        add(own0, tiles, c0, c1, P.shared_slots * P.shared.slot_tiles * P.shared.slot_rows + int64_t(item) * step + tb * P.own.slot_rows, step, P.own.slot_rows, row);
         const bool none = sum == 0.f;
         const float inv = none ? 0.f : 1.f / sum;
-        const int n = P.group.quot(first + row), h = hk * P.group.d + (first + row - n * P.group.d);
         T *dst = static_cast<T *>(A.out.data) + b * A.out.seq + n * A.out.node + h * A.out.head + lane * E;
 #pragma unroll
         for (int i = 0; i < E; i += 2) *reinterpret_cast<uint32_t *>(dst + i) = pack2<T>(o[i] * inv, o[i + 1] * inv);

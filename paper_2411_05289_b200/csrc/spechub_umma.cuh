@@ -16,6 +16,9 @@ __device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) {
 __device__ __forceinline__ void bar_arrive(uint32_t bar) {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
+__device__ __forceinline__ void bar_arrive(uint32_t bar, uint32_t count) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
 __device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
@@ -29,19 +32,21 @@ constexpr long long kWaitClocks = 4000000000ll;   // two seconds and more; no wa
 
 // Wait for a phase, for kWaitClocks at most.  When a wait runs out, `gave_up` (shared memory) is set; every wait of the CTA then
 // returns at once, so that the kernel runs to its end (over data that is not valid, within its bounds) and can say so.
-// Called by whole warps, which are together again afterwards.
-__device__ __forceinline__ void bar_wait(uint32_t bar, uint32_t parity, volatile int *gave_up) {
-    if (!bar_try(bar, parity)) {
-        const long long t0 = clock64();
-        for (unsigned polls = 1; !bar_try(bar, parity); ++polls) {
-            if (polls % 64 != 0) continue;
-            if (*gave_up) break;
-            if (clock64() - t0 > kWaitClocks) {
-                *gave_up = 1;
-                break;
-            }
+__device__ __forceinline__ void bar_wait_one(uint32_t bar, uint32_t parity, volatile int *gave_up) {
+    if (bar_try(bar, parity)) return;
+    const long long t0 = clock64();
+    for (unsigned polls = 1; !bar_try(bar, parity); ++polls) {
+        if (polls % 64 != 0) continue;
+        if (*gave_up) return;
+        if (clock64() - t0 > kWaitClocks) {
+            *gave_up = 1;
+            return;
         }
     }
+}
+// ... for whole warps, which are together again afterwards.
+__device__ __forceinline__ void bar_wait(uint32_t bar, uint32_t parity, volatile int *gave_up) {
+    bar_wait_one(bar, parity, gave_up);
     __syncwarp();
 }
 
@@ -50,6 +55,17 @@ __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap *map, i
     asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
                  ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar) : "memory");
 }
+// ... out of shared memory (what is out of range is left out); and plain bytes.  Stores are counted in groups of the issuing thread.
+__device__ __forceinline__ void tma_store(const CUtensorMap *map, uint32_t src, int x, int y, int z, int w) {
+    asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4, %5}], [%1];"
+                 ::"l"(map), "r"(src), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+__device__ __forceinline__ void bulk_store(void *dst, uint32_t src, uint32_t bytes) {
+    asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void store_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void store_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }   // shared memory may change
+__device__ __forceinline__ void store_wait() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 __device__ __forceinline__ void tma_prefetch_map(const CUtensorMap *map) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
 }
@@ -63,24 +79,21 @@ constexpr uint32_t kOperandHigh = 2u << 29 | 1u << 14 | 1024u >> 4;
 __host__ __device__ constexpr uint32_t mma_desc(bool bf16, int n, bool b_rows_along_n) {
     return (1u << 4) | (bf16 ? (1u << 7) | (1u << 10) : 0u) | (b_rows_along_n ? 1u << 16 : 0u) | (static_cast<uint32_t>(n / 8) << 17) | (8u << 24);
 }
-// d (tensor memory, 128 x n) = a b (+ d), 16 elements of K.  The whole warp comes here, with the same values, and the one thread for
-// which `lead` holds issues: without a branch around it the operands stay in uniform registers (100 -> 64 clocks per instruction).
-__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t desc, bool add, bool lead) {
-    asm volatile("{ .reg .pred p, q; .reg .b64 x, y; mov.b64 x, {%1, %5}; mov.b64 y, {%2, %5}; setp.ne.u32 p, %4, 0; setp.ne.u32 q, %6, 0; "
-                 "@q tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, p; }"
-                 ::"r"(d), "r"(a), "r"(b), "r"(desc), "r"(static_cast<uint32_t>(add)), "r"(kOperandHigh), "r"(static_cast<uint32_t>(lead)) : "memory");
+// d (tensor memory, 128 x n) = a b (+ d), 16 elements of K; one thread issues
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t desc, bool add) {
+    asm volatile("{ .reg .pred p; .reg .b64 x, y; mov.b64 x, {%1, %5}; mov.b64 y, {%2, %5}; setp.ne.u32 p, %4, 0; "
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, p; }"
+                 ::"r"(d), "r"(a), "r"(b), "r"(desc), "r"(static_cast<uint32_t>(add)), "r"(kOperandHigh) : "memory");
 }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t desc, bool add, bool lead) {   // a in tensor memory
-    asm volatile("{ .reg .pred p, q; .reg .b64 y; mov.b64 y, {%2, %5}; setp.ne.u32 p, %4, 0; setp.ne.u32 q, %6, 0; "
-                 "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %3, p; }"
-                 ::"r"(d), "r"(a), "r"(b), "r"(desc), "r"(static_cast<uint32_t>(add)), "r"(kOperandHigh), "r"(static_cast<uint32_t>(lead)) : "memory");
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t desc, bool add) {   // a in tensor memory
+    asm volatile("{ .reg .pred p; .reg .b64 y; mov.b64 y, {%2, %5}; setp.ne.u32 p, %4, 0; "
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %3, p; }"
+                 ::"r"(d), "r"(a), "r"(b), "r"(desc), "r"(static_cast<uint32_t>(add)), "r"(kOperandHigh) : "memory");
 }
 // the barrier gets an arrival when everything that this thread has issued to the tensor core is done
-__device__ __forceinline__ void mma_commit(uint32_t bar, bool lead) {
-    asm volatile("{ .reg .pred q; setp.ne.u32 q, %1, 0; @q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0]; }"
-                 ::"r"(bar), "r"(static_cast<uint32_t>(lead)) : "memory");
+__device__ __forceinline__ void mma_commit(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
-__device__ __forceinline__ int uniform(int v) { return __shfl_sync(kFull, v, 0); }   // says so to the compiler
 
 // 32 columns of the warp's 32 lanes, not waited for
 __device__ __forceinline__ void tmem_ld32_async(uint32_t taddr, float *v) {

@@ -266,12 +266,40 @@ def test_append_leaves_bad_pages_out(sh):
     ([100] * 9, 31, 1, 4, 128, 64, "hnd", 1000),
     ([5, -1, 600, -1], 3, 2, 7, 64, 32, "nhd", 333),
     ([0] * 200, 1, 2, 1, 64, 8, "nhd", 65),
+    ([70, 300], 5, 2, 33, 128, 16, "nhd", 0),              # tiles of 99 rows
+    ([600], 2, 1, 128, 64, 32, "hnd", 0),
 ])
 def test_attention(sh, dt, lens, n, hk, g, d, ps, layout, shared):
     c = Case(10 + n, lens, n, hk, g, d, ps, dt, layout, shared, tree_mask(n), strided_q=True)
     got = c.run(sh)
     assert got["status"].tolist() == [0] * len(lens)
     c.check(got)
+
+
+@pytest.mark.parametrize("lens,n,hk,g,d,shared", [
+    ([40, 7, 300, 0, 12], 7, 2, 4, 128, 300),       # four sequences' rows in a tile
+    ([5, 60, 2], 31, 1, 4, 64, 129),                # one
+    ([5, -1, 200], 40, 1, 7, 128, 700),             # a sequence's rows in several tiles
+    ([1, 2, 3] * 30, 1, 1, 8, 64, 1000),
+    ([50, 9], 3, 1, 128, 64, 64),                   # a node's heads are a tile
+])
+def test_queries_with_gaps_between_sequences(sh, lens, n, hk, g, d, shared):
+    """... and between nodes and heads: sequences do not follow each other as their nodes do."""
+    c = Case(50, lens, n, hk, g, d, 16, "bf16", "nhd", shared, tree_mask(n))
+    packed = c.run(sh)
+    c.check(packed)
+    wide = torch.full((len(lens) + 1, n + 2, hk * g + 3, d + 8), math.nan, dtype=c.dt, device="cuda")
+    wide[1:, 1:-1, 2:-1, :d] = c.q
+    c.q = wide[1:, 1:-1, 2:-1, :d]
+    got = c.run(sh)
+    c.check(got)
+    room = torch.full_like(wide, 3.0)
+    view = room[1:, 1:-1, 2:-1, :d]
+    c.run(sh, out=dict(out=view, lse=torch.empty_like(got["lse"]), status=torch.empty_like(got["status"])))
+    for i, x in enumerate(lens):
+        assert torch.equal(view[i], got["out"][i] if x >= 0 else torch.full_like(view[i], 3.0))
+    view.fill_(3.0)
+    assert bool((room == 3.0).all())    # nothing is written beside the rows
 
 
 @pytest.mark.parametrize("dt", ["bf16", "fp16"])
