@@ -13,15 +13,19 @@
 // is finished in place; other pieces go to the workspace and attention_join_kernel adds them in the order of the CTAs.
 //
 // CTA.  Warp 8 brings queries and keys, warp 11 values (bulk tensor copies, a box per page and 64 dimensions, each through a ring of its
-// own), one thread of warp 9 issues the matrix instructions, warps 0-3 and 4-7 are two softmax groups, a row per thread, each with its
-// own S, P and O in tensor memory.  Two tiles of 128 rows: each group has one of them and every K / V tile serves both.  One: the groups
-// take the K / V tiles in turn, for the same rows, and are joined at the end of the piece; else the tensor core and the loads would
-// wait while one group computes.  P takes the place of S (head_dim 64 has room for its own).  A single warp gets through an instruction
-// in 4 to 5 clocks, so what the single warps and the turnover between pieces do is kept short: queries and outputs are copied as tensors
-// too (a box of all heads of some nodes), pieces of the workspace as they lie in shared memory, and the next piece is looked up early.
+// own), warps 0-3 and 4-7 are two softmax groups, a row per thread, each with its own S, P and O in tensor memory and a thread of its own
+// (of warps 9 and 10) that issues its matrix instructions.  Two tiles of 128 rows: each group has one of them and every K / V tile serves
+// both.  One: the groups take the K / V tiles in turn, for the same rows, and are joined at the end of the piece; else the tensor core
+// and the loads would wait while one group computes.  P takes the place of S (head_dim 64 has room for its own).
+//
+// A single warp gets through an instruction in 4 to 5 clocks, and more when the others' code pushes its own out of the instruction
+// cache.  So what single warps and the turnover between pieces do is kept short: queries and outputs are copied as tensors too (a box of
+// all heads of some nodes), pieces of the workspace as they lie in shared memory; warp 8 alone finds the pieces, ahead of the others.
+// One thread for the matrix instructions of both groups was late for each of them (4400 clocks for 256 rows and 128 keys, of which the
+// tensor core needs 2050).
 //
 // What lies behind a sequence's end in a page may be anything.  Its scores are replaced, and its values, and values of tree nodes
-// that are no finite numbers, are cleared in shared memory before the product (by warp 10), since 0 * NaN would reach every row; the
+// that are no finite numbers, are cleared in shared memory before the product (by the softmax group whose weights they meet), since 0 * NaN would reach every row; the
 // rows that do see such a node get it added at the end.
 #pragma once
 
@@ -33,6 +37,7 @@ namespace spechub {
 
 constexpr int kTile = 128;         // keys of a tile, rows of a softmax group
 constexpr int kAttThreads = 384;
+constexpr int kPieces = 4, kPieceReaders = 11;   // pieces that are known ahead; who reads them: 8 softmax warps, warps 9 to 11
 // Registers of a thread: what the block is launched with, and how its warpgroups share them then (a row of scores is 128).
 constexpr int kLaunchRegs = 168, kSoftmaxRegs = 200, kOtherRegs = 104;
 static_assert(256 * kSoftmaxRegs + 128 * kOtherRegs <= kAttThreads * kLaunchRegs, "the block's own registers");
@@ -48,9 +53,8 @@ struct AttShape {
     static constexpr int kHalves = D / 64;
     static constexpr int kHalfBytes = kTile * 128;                   // 128 rows of 64 elements
     static constexpr int kTileBytes = kHalves * kHalfBytes;          // a tile of keys, of values, or of queries
-    static constexpr int kKeyStages = D == 64 ? 5 : 2, kValueStages = D == 64 ? 5 : 3;
-    // Outputs leave through 4 KB per softmax warp: for heads of 128 in the place of the piece's queries, which are 32 KB a tile.
-    static constexpr int kStaging = D == 64 ? 8 * 4096 : 0;
+    static constexpr int kKeyStages = D == 64 ? 4 : 2, kValueStages = D == 64 ? 4 : 2;   // powers of two
+    static constexpr int kStaging = 2 * kHalfBytes;                  // outputs leave through 16 KB of each group
     static constexpr int kSmem = (2 + kKeyStages + kValueStages) * kTileBytes + kStaging + 1024;  // (1024: alignment)
     // columns of tensor memory
     static constexpr int kS = 0, kO = 256, kP = D == 64 ? 384 : 0, kPStep = D == 64 ? 64 : 128;
@@ -127,7 +131,7 @@ struct AttPiece {
     __device__ bool masked(int t) const { return t >= plain / kTile; }
 };
 
-// The pieces of a CTA's run; every role walks through them by itself.
+// The pieces of a CTA's run, one after the other (warp 8 does this and tells the others).
 struct AttStart { int from, to, at; bool shared; int b, head, block; };   // costs; `at`: where the block begins
 struct AttWalk {
     const CacheArgs &c;
@@ -194,7 +198,8 @@ __device__ __forceinline__ AttTile tile_of(const AttKernelArgs &K, bool shared, 
 }
 
 // Bits of the keys of a masked tile that a row sees (bit j of word w: key 128 t + 32 w + j).
-__device__ __forceinline__ void row_bits(const AttentionArgs &A, const AttPiece &x, int t, int n, uint32_t (&bits)[4]) {
+__device__ __noinline__ uint4 row_bits(const AttentionArgs &A, const AttPiece &x, int t, int n) {
+    uint32_t bits[4];
     const int words = (A.c.nodes + 31) / 32;
     const int32_t *mask = A.mask + x.b * A.mask_stride_seq + n * static_cast<int64_t>(words);
 #pragma unroll
@@ -213,6 +218,21 @@ __device__ __forceinline__ void row_bits(const AttentionArgs &A, const AttPiece 
         if (at + 32 > x.keys) m &= at >= x.keys ? 0u : (1u << (x.keys - at)) - 1;   // (the masks' bits behind the last node may be anything)
         bits[w] = m;
     }
+    return make_uint4(bits[0], bits[1], bits[2], bits[3]);
+}
+
+// A row's scores that it does not see, in tensor memory: -inf.
+__device__ __noinline__ void mask_scores(uint32_t t_s, uint4 bits) {
+#pragma unroll 1
+    for (int h = 0; h < 4; ++h) {
+        float s[32];
+        tmem_ld32(t_s + 32 * h, s);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) s[i] = bits.x >> i & 1 ? s[i] : neg_inf();
+        tmem_st32(t_s + 32 * h, s);
+        bits = make_uint4(bits.y, bits.z, bits.w, 0);
+    }
+    tmem_wait_st();
 }
 
 template <class T> __device__ __forceinline__ bool not_finite(uint16_t e);
@@ -239,18 +259,46 @@ __device__ __noinline__ void add_not_finite(const AttentionArgs &A, const AttPie
     }
 }
 
+// A tile of values in shared memory, looked through by 128 threads: rows from r1 become zero, and in rows r0..r1 what is no finite number.
+// true: this thread found such.
+template <class T, int D>
+__device__ __noinline__ bool clear_values(uint8_t *v, int thread, int r0, int r1) {
+    constexpr int kVecs = D / 8;
+    constexpr uint32_t kExp = Weight<T>::kBf16 ? 0x7f807f80u : 0x7c007c00u;   // all ones: no finite number
+    const auto place = [&](int i) { return reinterpret_cast<uint4 *>(v + (i % kVecs / 8) * (kTile * 128) + (i / kVecs) * 128 + (i % 8) * 16); };
+    for (int i = thread + r1 * kVecs; i < kTile * kVecs; i += kTile) *place(i) = make_uint4(0, 0, 0, 0);
+    bool bad = false;
+#pragma unroll 4
+    for (int i = thread + r0 * kVecs; i < r1 * kVecs; i += kTile) {
+        uint4 u = *place(i);
+        uint32_t most = __vimax3_u16x2(u.x & 0x7fff7fffu, u.y & 0x7fff7fffu, u.z & 0x7fff7fffu);   // magnitudes as numbers of 15 bits
+        most = __vmaxu2(most, u.w & 0x7fff7fffu);
+        if ((most & 0xffffu) < (kExp & 0xffffu) && most >> 16 < kExp >> 16) continue;
+        uint32_t *w = &u.x;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if ((w[k] & kExp & 0xffffu) == (kExp & 0xffffu)) w[k] &= 0xffff0000u;
+            if ((w[k] & kExp & 0xffff0000u) == (kExp & 0xffff0000u)) w[k] &= 0xffffu;
+        }
+        *place(i) = u;
+        bad = true;
+    }
+    return bad;
+}
+
 template <class T, int D>
 __global__ void __launch_bounds__(kAttThreads, 1) attention_kernel(const __grid_constant__ AttKernelArgs K, const __grid_constant__ AttMaps maps) {
     using L = AttShape<D>;
     constexpr bool kBf16 = Weight<T>::kBf16;
     constexpr int SK = L::kKeyStages, SV = L::kValueStages;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ __align__(8) uint64_t bars[2 * (SK + SV) + 13];
+    __shared__ __align__(8) uint64_t bars[2 * (SK + SV) + 16 + 2 * kPieces];
     __shared__ uint32_t tmem_base;
     __shared__ int gave_up_, bad_values;
     __shared__ float2 other[kTile];           // of each row: (reference, sum) of group 1, then both groups' factors
     __shared__ int warp_sum[kAttThreads / 32];
     __shared__ AttStart start;
+    __shared__ AttPiece pieces[kPieces];      // the next ones; t1 = 0: there are no more
     volatile int *const gave_up = &gave_up_;
 
     const AttentionArgs &A = K.a;
@@ -258,7 +306,7 @@ __global__ void __launch_bounds__(kAttThreads, 1) attention_kernel(const __grid_
     const AttPlan &P = K.p;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     uint8_t *const smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    const uint32_t s_q = saddr(smem), s_k = s_q + 2 * L::kTileBytes, s_v = s_k + SK * L::kTileBytes, bar0 = saddr(bars);
+    const uint32_t s_q = saddr(smem), s_k = s_q + 2 * L::kTileBytes, s_v = s_k + SK * L::kTileBytes, s_out = s_v + SV * L::kTileBytes, bar0 = saddr(bars);
     const auto k_full = [&](int s) { return bar0 + 8u * s; };
     const auto k_empty = [&](int s) { return bar0 + 8u * (SK + s); };
     const auto v_full = [&](int s) { return bar0 + 8u * (2 * SK + s); };
@@ -269,19 +317,26 @@ __global__ void __launch_bounds__(kAttThreads, 1) attention_kernel(const __grid_
     const auto s_full = [&](int t) { return bar1 + 32u + 8u * t; };
     const auto p_full = [&](int t) { return bar1 + 48u + 8u * t; };
     const auto o_full = [&](int t) { return bar1 + 64u + 8u * t; };
-    const uint32_t o_free = bar1 + 80u, v_here = bar1 + 88u, v_clean = bar1 + 96u;
+    const uint32_t o_free = bar1 + 80u;
+    const auto meet = [&](int i) { return bar1 + 88u + 8u * i; };   // of softmax warps: of all, of either group
+    const auto turn = [&](int t) { return bar1 + 112u + 8u * t; };   // at the tensor core
+    const auto piece_full = [&](int i) { return bar1 + 128u + 8u * i; };
+    const auto piece_empty = [&](int i) { return bar1 + 128u + 8u * (kPieces + i); };
 
     if (warp == 9) tmem_alloc(saddr(&tmem_base), 512);
     if (tid == 0) {
-        for (int s = 0; s < SK; ++s) { bar_init(k_full(s), 1); bar_init(k_empty(s), 1); }
-        for (int s = 0; s < SV; ++s) { bar_init(v_full(s), 1); bar_init(v_empty(s), 1); }
+        for (int s = 0; s < SK; ++s) { bar_init(k_full(s), 1); bar_init(k_empty(s), 2); }
+        for (int s = 0; s < SV; ++s) { bar_init(v_full(s), 1); bar_init(v_empty(s), 2); }
         for (int t = 0; t < 2; ++t) {
-            bar_init(q_full(t), 1); bar_init(q_empty(t), 8);
-            bar_init(s_full(t), 1); bar_init(p_full(t), kTile); bar_init(o_full(t), 1);
+            bar_init(q_full(t), 1); bar_init(q_empty(t), 2);
+            bar_init(s_full(t), 1); bar_init(p_full(t), 4); bar_init(o_full(t), 1);
+            bar_init(turn(t), 1);
         }
-        bar_init(o_free, 2 * kTile);
-        bar_init(v_here, 1);
-        bar_init(v_clean, 1);
+        bar_init(o_free, 8);
+        bar_init(meet(0), 8);
+        bar_init(meet(1), 4);
+        bar_init(meet(2), 4);
+        for (int i = 0; i < kPieces; ++i) { bar_init(piece_full(i), 1); bar_init(piece_empty(i), kPieceReaders); }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         gave_up_ = 0;
         bad_values = 0;
@@ -348,8 +403,17 @@ __global__ void __launch_bounds__(kAttThreads, 1) attention_kernel(const __grid_
         tmem_fence_after();
     }
     const uint32_t tm = tmem_base;
-    AttWalk walk(K, start);
     AttPiece x = {};
+    int piece_slot = 0;
+    uint32_t piece_phase = 0;
+    const auto next_piece = [&](AttPiece &y) {   // one arrival per reader: a warp, or a thread of warps 9 and 10
+        bar_wait_one(piece_full(piece_slot), piece_phase, gave_up);
+        y = pieces[piece_slot];
+        if (warp < 8 || warp == 11) __syncwarp();
+        if (lane == 0) bar_arrive(piece_empty(piece_slot));
+        if (++piece_slot == kPieces) { piece_slot = 0; piece_phase ^= 1u; }
+        return y.t1 > 0 && *gave_up == 0;
+    };
 
     if (warp < 8) {
         // ---- softmax ---------------------------------------------------------------------------------
@@ -357,10 +421,17 @@ __global__ void __launch_bounds__(kAttThreads, 1) attention_kernel(const __grid_
         const int g = warp >> 2, gt = tid & (kTile - 1);
         const uint32_t lanes = static_cast<uint32_t>(32 * (warp & 3)) << 16;
         const uint32_t t_s = tm + lanes + L::kS + g * kTile, t_p = tm + lanes + L::kP + g * L::kPStep, t_o = tm + lanes + L::kO;
-        uint32_t s_phase = 0, o_phase = 0;
-        int q_slot = 0;
+        uint32_t s_phase = 0, o_phase = 0, meet_phase[2] = {0, 0};
+        const auto together = [&](bool all) {   // (with an end, unlike the hardware's barriers: a warp may have given up)
+            __syncwarp();
+            const uint32_t bar = meet(all ? 0 : 1 + g);
+            if (lane == 0) bar_arrive(bar);
+            bar_wait(bar, meet_phase[all], gave_up);
+            meet_phase[all] ^= 1u;
+        };
         const float cs = A.scale_log2;
-        bool there = walk.next(x);
+        uint32_t n0 = 0;   // tiles of values before this piece
+        bool there = next_piece(x);
         while (there) {
             const int tile = 2 * x.block + (x.two ? g : 0);
             const AttTile rows = tile_of(K, x.shared, tile);
@@ -370,27 +441,30 @@ __global__ void __launch_bounds__(kAttThreads, 1) attention_kernel(const __grid_
             const int step = x.two ? 1 : 2, first = x.two ? x.t0 : x.t0 + g;
             for (int t = first; t < x.t1; t += step) {
                 const bool masked = x.masked(t);
-                uint32_t bits[4] = {};
-                if (masked && warp_on) row_bits(A, x, t, x.shared ? 0 : rows.node + min(in, rows.count - 1), bits);
+                uint4 bits = {};
+                if (masked && warp_on) bits = row_bits(A, x, t, x.shared ? 0 : rows.node + min(in, rows.count - 1));
                 bar_wait(s_full(g), s_phase, gave_up);
                 s_phase ^= 1u;
                 tmem_fence_after();
                 if (warp_on) {
-                    float s[kTile];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) tmem_ld32_async(t_s + 32 * i, s + 32 * i);
-                    tmem_wait_ld(s);
-                    if (masked) {
-#pragma unroll
-                        for (int i = 0; i < kTile; ++i) s[i] = bits[i / 32] >> (i & 31) & 1 ? s[i] : neg_inf();
-                    }
+                    // Loops, and what is rare in functions: in one stretch of code, with all 128 scores in registers, a tile takes 1380
+                    // clocks where it is alone and 1680 as here, but here the warps wait less for their code (502 -> 372 us for 64 x 31
+                    // nodes behind 8192 shared tokens).  Exponentials by a polynomial, for a part of them, bring nothing here.
+                    if (masked) mask_scores(t_s, bits);
                     float m0 = neg_inf(), m1 = neg_inf(), m2 = neg_inf(), m3 = neg_inf();
+#pragma unroll 1
+                    for (int h = 0; h < 2; ++h) {
+                        float s[64];
+                        tmem_ld32_async(t_s + 64 * h, s);
+                        tmem_ld32_async(t_s + 64 * h + 32, s + 32);
+                        tmem_wait_ld(s);
 #pragma unroll
-                    for (int i = 0; i < kTile; i += 8) {
-                        m0 = max3(m0, s[i], s[i + 1]);
-                        m1 = max3(m1, s[i + 2], s[i + 3]);
-                        m2 = max3(m2, s[i + 4], s[i + 5]);
-                        m3 = max3(m3, s[i + 6], s[i + 7]);
+                        for (int i = 0; i < 64; i += 8) {
+                            m0 = max3(m0, s[i], s[i + 1]);
+                            m1 = max3(m1, s[i + 2], s[i + 3]);
+                            m2 = max3(m2, s[i + 4], s[i + 5]);
+                            m3 = max3(m3, s[i + 6], s[i + 7]);
+                        }
                     }
                     const float top = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3)) * cs - Weight<T>::kBias;
                     if (t == first) ref = top;
@@ -400,41 +474,57 @@ __global__ void __launch_bounds__(kAttThreads, 1) attention_kernel(const __grid_
                         sum *= f;
                         ref = now;
 #pragma unroll 1
-                        for (int i = 0; i < D; i += 32) {
-                            float o[32];
-                            tmem_ld32(t_o + g * D + i, o);
+                        for (int i = 0; i < D; i += 8) {   // (few at a time: the scores are in registers)
+                            float o[8];
+                            tmem_ld8(t_o + g * D + i, o);
 #pragma unroll
-                            for (int j = 0; j < 32; ++j) o[j] *= f;
-                            tmem_st32(t_o + g * D + i, o);
+                            for (int j = 0; j < 8; ++j) o[j] *= f;
+                            tmem_st8(t_o + g * D + i, o);
                         }
                     }
                     const float sub = ref == neg_inf() ? 0.f : -ref;
-                    const float2 cs2 = make_float2(cs, cs), sub2 = make_float2(sub, sub);
+                    const float2 sub2 = make_float2(sub, sub), cs2 = make_float2(cs, cs);
                     float2 l0 = make_float2(0.f, 0.f), l1 = l0;
+#pragma unroll 1
+                    for (int h = 0; h < 2; ++h) {
+                        float s[64];
+                        tmem_ld32_async(t_s + 64 * h, s);
+                        tmem_ld32_async(t_s + 64 * h + 32, s + 32);
+                        tmem_wait_ld(s);
 #pragma unroll
-                    for (int h = 0; h < 4; ++h) {
-                        uint32_t w[16];
+                        for (int q = 0; q < 2; ++q) {
+                            uint32_t w[16];
 #pragma unroll
-                        for (int i = 0; i < 16; i += 2) {
-                            const float *y = s + 32 * h + 2 * i;
-                            const float2 a = fma2(make_float2(y[0], y[1]), cs2, sub2), b = fma2(make_float2(y[2], y[3]), cs2, sub2);
-                            const float2 e = make_float2(ex2(a.x), ex2(a.y)), f = make_float2(ex2(b.x), ex2(b.y));
-                            l0 = add2(l0, e);
-                            l1 = add2(l1, f);
-                            w[i] = pack2<T>(e.x, e.y);
-                            w[i + 1] = pack2<T>(f.x, f.y);
+                            for (int i = 0; i < 16; ++i) {
+                                const float2 a = fma2(make_float2(s[32 * q + 2 * i], s[32 * q + 2 * i + 1]), cs2, sub2);
+                                const float2 e = make_float2(ex2(a.x), ex2(a.y));
+                                if (i & 1) l1 = add2(l1, e);
+                                else l0 = add2(l0, e);
+                                w[i] = pack2<T>(e.x, e.y);
+                            }
+                            tmem_st16_async(t_p + 32 * h + 16 * q, w);   // (over scores that have been read)
                         }
-                        tmem_st16_async(t_p + 16 * h, w);
                     }
                     sum += (l0.x + l0.y) + (l1.x + l1.y);
                     tmem_wait_st();
                     tmem_fence_before();
                 }
-                bar_arrive(p_full(g));
+                if (masked) {
+                    // Values behind the end, and those of tree nodes that are no numbers: zero.  (Both groups do it where both have the tile;
+                    // the ring is neither before nor behind this place: these scores came after the last products, these weights are waited for.)
+                    const uint32_t n = n0 + t - x.t0;
+                    bar_wait(v_full(n % SV), n / SV & 1u, gave_up);
+                    if (clear_values<T, D>(smem + (2 + SK + n % SV) * L::kTileBytes, gt, max(0, x.plain - t * kTile), min(kTile, x.keys - t * kTile)))
+                        *static_cast<volatile int *>(&bad_values) = 1;   // (from here on the CTA looks for such nodes)
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __threadfence_block();
+                }
+                __syncwarp();
+                if (lane == 0) bar_arrive(p_full(g));
             }
             // ---- the end of the piece ------------------------------------------------------------------
             AttPiece y = {};
-            there = walk.next(y);   // (while the last product runs)
+            there = next_piece(y);   // (while the last product runs)
             if (first < x.t1) {
                 bar_wait(o_full(g), o_phase, gave_up);
                 o_phase ^= 1u;
@@ -445,7 +535,7 @@ __global__ void __launch_bounds__(kAttThreads, 1) attention_kernel(const __grid_
             if (!x.two) {   // the groups have the same rows, and each writes half of the columns
                 if (g == 1) other[gt] = make_float2(ref, sum);
                 tmem_fence_before();
-                asm volatile("bar.sync 1, 256;" ::: "memory");
+                together(true);
                 if (g == 0 && join) {
                     const float2 z = other[gt];
                     const float both = fmaxf(ref, z.x), r = both == neg_inf() ? 0.f : both;
@@ -461,31 +551,38 @@ __global__ void __launch_bounds__(kAttThreads, 1) attention_kernel(const __grid_
             }
             if (!x.two) {
                 if (g == 0) other[gt] = make_float2(f0, f1);
-                asm volatile("bar.sync 1, 256;" ::: "memory");
+                together(true);
                 if (g == 1) { const float2 z = other[gt]; f0 = z.x; f1 = z.y; }
             }
             tmem_fence_after();
-            const int slot0 = q_slot, slot1 = q_slot ^ 1;   // of queries
             const uint32_t o0 = t_o + (x.two ? g * D : 0);
             const int col0 = x.two ? 0 : g * (D / 2), col1 = x.two ? D : col0 + D / 2;
-            const int row_in = 32 * (warp & 3) + lane;
+            // 64 columns of a finished tile are in shared memory: on their way
+            const auto half_done = [&](int half) {
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                const bool both = D == 64 && !x.two;   // (each group has 32 of them)
+                together(both);
+                if (lane == 0 && (warp & 3) == 0 && !(both && g)) {
+                    tma_store(&maps.out, s_out + (both ? 0 : g * L::kHalfBytes), 64 * half, x.head * P.group.d, rows.node, x.b);
+                    store_commit();
+                    store_wait_read();
+                }
+                if (x.two && half == 0 && D == 128) together(false);   // (the second half goes the same way)
+            };
             if (warp_on) {
                 const int bad = *static_cast<volatile int *>(&bad_values);
                 const AttRows &r = x.shared ? P.shared : P.own;
-                int64_t slot_tile = 0;   // tile of rows in the workspace, counted in such tiles
+                int64_t row0 = 0;   // in the workspace
                 if (!whole) {
-                    slot_tile = (x.item + int64_t(blockIdx.x)) * r.slot_tiles + (x.two ? g : 0);
-                    const int64_t row0 = x.shared ? slot_tile * r.slot_rows : P.shared_slots * P.shared.slot_tiles * P.shared.slot_rows + slot_tile * r.slot_rows;
-                    slot_tile = row0;
+                    row0 = ((x.item + int64_t(blockIdx.x)) * r.slot_tiles + (x.two ? g : 0)) * r.slot_rows +
+                           (x.shared ? 0 : P.shared_slots * P.shared.slot_tiles * P.shared.slot_rows);
                     if (mine && (x.two || g == 0)) P.ml[row0 + gt] = make_float2(ref, sum);
                 } else if (mine && A.lse && (x.two || g == 0)) {
                     A.lse[(static_cast<int64_t>(x.b) * c.nodes + rows.node + in) * c.heads + x.head * P.group.d + (gt - in * P.group.d)] =
                         none ? neg_inf() : (ref + log2f(sum)) * 0.6931471805599453f;
                 }
-                // 4 KB (two of them for a group that is alone in 32) of this warp
-                const uint32_t tile_at = D == 64 ? s_v + SV * L::kTileBytes + (x.two ? g : 0) * L::kTileBytes : s_q + (x.two && g ? slot1 : slot0) * L::kTileBytes;
-                const uint32_t own_at = D == 64 ? s_v + SV * L::kTileBytes + 4096 * warp
-                                                : tile_at + (x.two ? 8192 * (warp & 3) : 4096 * warp);
+                // 16 KB of staging per group: 64 columns of a tile as its type, or 4 KB of each warp
+                const uint32_t half_at = s_out + (D == 64 && !x.two ? 0 : g * L::kHalfBytes), own_at = s_out + 4096 * warp;
                 const uint32_t lane_rows = min(32, valid - (gt - lane));
 #pragma unroll 1
                 for (int i = col0; i < col1; i += 32) {
@@ -509,62 +606,132 @@ __global__ void __launch_bounds__(kAttThreads, 1) attention_kernel(const __grid_
                     }
                     __syncwarp();
                     if (whole) {
-                        const uint32_t at = tile_at + (i / 64) * L::kHalfBytes + row_in * 128;
+                        const uint32_t at = half_at + gt * 128;
+                        if ((i & 32) == 0 && i > col0) half_done(i / 64 - 1);   // (a group that is alone: its first half goes before)
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
                             const float *y8 = o + 8 * j;
-                            st_shared(at + (((i & 32) / 8 + j) ^ (row_in & 7)) * 16, pack2<T>(y8[0], y8[1]), pack2<T>(y8[2], y8[3]),
+                            st_shared(at + (((i & 32) / 8 + j) ^ (gt & 7)) * 16, pack2<T>(y8[0], y8[1]), pack2<T>(y8[2], y8[3]),
                                       pack2<T>(y8[4], y8[5]), pack2<T>(y8[6], y8[7]));
                         }
                     } else {
-                        const uint32_t at = own_at + (D == 128 && x.two ? (i & 32) * 128 : 0);
-                        if (lane == 0 && (D == 64 || !x.two || (i & 32) == 0)) store_wait_read();
+                        if (lane == 0) store_wait_read();
                         __syncwarp();
 #pragma unroll
                         for (int j = 0; j < 8; ++j)
-                            st_shared(at + lane * 128 + (j ^ (lane & 7)) * 16, __float_as_uint(o[4 * j]), __float_as_uint(o[4 * j + 1]), __float_as_uint(o[4 * j + 2]),
+                            st_shared(own_at + lane * 128 + (j ^ (lane & 7)) * 16, __float_as_uint(o[4 * j]), __float_as_uint(o[4 * j + 1]), __float_as_uint(o[4 * j + 2]),
                                       __float_as_uint(o[4 * j + 3]));
                         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                         __syncwarp();
                         if (lane == 0) {
-                            bulk_store(P.o + slot_tile * D + (i / 32) * int64_t(r.slot_rows) * 32 + (gt - lane) * 32, at, lane_rows * 128);
+                            bulk_store(P.o + row0 * D + (i / 32) * int64_t(r.slot_rows) * 32 + (gt - lane) * 32, own_at, lane_rows * 128);
                             store_commit();
                         }
                     }
                 }
-            }
+            } else if (whole && x.two && D == 128) half_done(0);
             tmem_fence_before();
-            bar_arrive(o_free);
-            if (whole) {
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                if (x.two && g == 0) asm volatile("bar.sync 2, 128;" ::: "memory");
-                else if (x.two) asm volatile("bar.sync 3, 128;" ::: "memory");
-                else asm volatile("bar.sync 1, 256;" ::: "memory");
-                if (lane == 0 && (x.two ? (warp & 3) == 0 : warp == 0)) {
-                    const uint32_t at = D == 64 ? s_v + SV * L::kTileBytes + (x.two ? g : 0) * L::kTileBytes : s_q + (x.two && g ? slot1 : slot0) * L::kTileBytes;
-                    for (int h = 0; h < L::kHalves; ++h) tma_store(&maps.out, at + h * L::kHalfBytes, 64 * h, x.head * P.group.d, rows.node, x.b);
-                    store_commit();
-                }
-            }
-            // the queries' slots may be filled again
-            if (lane == 0) {
-                store_wait_read();
-                if (x.two) bar_arrive(q_empty(g ? slot1 : slot0), 2);
-                else bar_arrive(q_empty(slot0), 1);
-            }
             __syncwarp();
-            if (!x.two) q_slot ^= 1;
+            if (lane == 0) bar_arrive(o_free);
+            if (whole) half_done(x.two ? L::kHalves - 1 : D == 64 ? 0 : g);
+            n0 += x.t1 - x.t0;
             x = y;
         }
         if (lane == 0) store_wait();
-    } else if (fewer_registers<kOtherRegs>(), warp == 8 || warp == 11) {
-        // ---- tiles of keys (warp 8, and queries) and values (warp 11) -------------------------------------------
-        const bool keys = warp == 8;
-        const int stages = keys ? SK : SV;
-        const uint32_t ring = keys ? s_k : s_v, full = keys ? k_full(0) : v_full(0), empty = keys ? k_empty(0) : v_empty(0);
-        const CUtensorMap *const map = keys ? &maps.k : &maps.v;
-        int stage = 0, q_slot = 0;
-        uint32_t phase = 1, q_phase = 1;
+    } else if (fewer_registers<kOtherRegs>(), warp == 9 || warp == 10) {
+        // ---- matrix instructions of a group: one thread ---------------------------------------------------
+        if (lane == 0) {
+            const int g = warp - 9;
+            uint32_t k_n = 0, v_n = 0, q_n = 0;   // tiles and slots gone by
+            uint32_t p_phase = 0, free_phase = 1, turn_phase = g == 0;
+            constexpr uint32_t desc_s = mma_desc(kBf16, kTile, false), desc_o = mma_desc(kBf16, D, true);
+            const uint32_t k_op = operand(s_k, L::kHalfBytes), v_op = operand(s_v, L::kHalfBytes), q_op = operand(s_q, L::kHalfBytes);
+            const uint32_t d_s = tm + L::kS + g * kTile, d_o = tm + L::kO + g * D, a_p = tm + L::kP + g * L::kPStep;
+            const auto k_arrived = [&]() { bar_wait_one(k_full(k_n % SK), k_n / SK & 1u, gave_up); };
+            const auto v_arrived = [&]() { bar_wait_one(v_full(v_n % SV), v_n / SV & 1u, gave_up); };
+            // tiles that are the other group's: both say when they have passed one, or a wait could take one time round the ring for another
+            const auto pass_k = [&](int upto) {
+                for (; static_cast<int>(k_n) < upto; ++k_n) { k_arrived(); bar_arrive(k_empty(k_n % SK)); }
+            };
+            const auto pass_v = [&](int upto) {
+                for (; static_cast<int>(v_n) < upto; ++v_n) { v_arrived(); bar_arrive(v_empty(v_n % SV)); }
+            };
+            int n0 = 0;   // tiles before this piece
+            while (next_piece(x)) {
+                const int n = x.t1 - x.t0, step = x.two ? 1 : 2, first = x.two ? 0 : g;
+                const uint32_t q = q_n + (x.two ? g : 0);   // the slot of queries
+                q_n += x.two ? 2 : 1;
+                if (x.two && g == 1) bar_wait_one(q_full((q - 1) & 1u), (q - 1) / 2 & 1u, gave_up);
+                bar_wait_one(q_full(q & 1u), q / 2 & 1u, gave_up);
+                if (x.two && g == 0) bar_wait_one(q_full((q + 1) & 1u), (q + 1) / 2 & 1u, gave_up);
+                // Two tiles of rows: the groups' products and scores go in turns, whole.  Mixed, both would be done at the same time, and
+                // both groups would then compute their weights at the same time, and the tensor core would wait for both (5400 clocks
+                // for a tile of keys; in turns 4100).
+                const auto my_turn = [&]() {
+                    if (!x.two) return;
+                    bar_wait_one(turn(g), turn_phase, gave_up);
+                    turn_phase ^= 1u;
+                };
+                bool o_mine = false;
+                for (int i = first - step; i < n; i += step) {
+                    const bool now = i >= first, more = i + step < n;
+                    if (now) {
+                        pass_v(n0 + i);
+                        v_arrived();
+                        if (!o_mine) {   // O of the piece before has been read by now or soon
+                            bar_wait_one(o_free, free_phase, gave_up);
+                            o_mine = true;
+                        }
+                    }
+                    const uint32_t v_slot = v_n % SV;
+                    if (more) pass_k(n0 + i + step);
+                    if (more && (x.two || !now)) k_arrived();   // (else the products first: these keys may still be on their way)
+                    if (now) {   // O (+)= P V
+                        const uint32_t b = v_op + v_slot * (L::kTileBytes >> 4);
+                        const bool add = i > first;
+                        bar_wait_one(p_full(g), p_phase, gave_up);
+                        p_phase ^= 1u;
+                        my_turn();
+                        tmem_fence_after();
+#pragma unroll
+                        for (int k = 0; k < kTile / 16; ++k) mma_ts(d_o, a_p + 8 * k, b + k * (2048 >> 4), desc_o, add || k > 0);
+                        ++v_n;
+                        if (!x.two) mma_commit(v_empty(v_slot));
+                    } else my_turn();
+                    if (more) {   // S = Q K^T
+                        if (now && !x.two) k_arrived();
+                        const uint32_t k_slot = k_n % SK, a = q_op + (q & 1u) * (L::kTileBytes >> 4), b = k_op + k_slot * (L::kTileBytes >> 4);
+#pragma unroll
+                        for (int k = 0; k < D / 16; ++k) {
+                            const uint32_t off = ((k / 4) * L::kHalfBytes + (k % 4) * 32) >> 4;
+                            mma_ss(d_s, a + off, b + off, desc_s, k > 0);
+                        }
+                        mma_commit(s_full(g));
+                        if (x.two) bar_arrive(turn(1 - g));
+                        mma_commit(k_empty(k_slot));
+                        ++k_n;
+                        if (i + 2 * step >= n) {   // the last ones
+                            mma_commit(q_empty(q & 1u));
+                            if (x.two) mma_commit(q_empty(q & 1u));
+                        }
+                    } else {
+                        if (now) mma_commit(o_full(g));
+                        if (x.two) bar_arrive(turn(1 - g));
+                    }
+                    if (now && x.two) mma_commit(v_empty(v_slot));
+                }
+                if (first >= n) bar_arrive(q_empty(q & 1u));
+                n0 += n;
+                pass_k(n0);
+                pass_v(n0);
+                if (!o_mine) bar_wait_one(o_free, free_phase, gave_up);
+                free_phase ^= 1u;
+            }
+            bar_wait_one(o_free, free_phase, gave_up);
+        }
+        __syncwarp();
+    } else {
+        // ---- tiles of keys, queries and pieces (warp 8); tiles of values (warp 11) ------------------------------
         const int ps = 1 << c.page_shift, box = min(ps, kTile), boxes = kTile / box;
         const auto page_at = [&](int t) -> int {   // lane i: the page of the tile's i-th box (c.pages: reads as zeros)
             const int slot = t * kTile + lane * box;
@@ -573,166 +740,79 @@ __global__ void __launch_bounds__(kAttThreads, 1) attention_kernel(const __grid_
             const int page = x.shared ? A.shared_table[at] : c.table[x.b * c.stride_table + at];   // (no key lies behind the table)
             return page >= 0 && page < c.pages ? page : c.pages;
         };
-        while (walk.next(x)) {
-            int page = page_at(x.t0);
-            for (int t = x.t0; t < x.t1; ++t) {
-                const int next = page_at(t + 1);
-                bar_wait(empty + 8 * stage, phase, gave_up);
-                if (lane == 0) bar_expect(full + 8 * stage, L::kTileBytes);
-                __syncwarp();
-                if (lane < boxes) {
-                    const uint32_t dst = ring + stage * L::kTileBytes + lane * box * 128;
-                    const int y = ps > kTile ? (t * kTile) & (ps - 1) : 0;
+        const auto bring = [&](const CUtensorMap *map, int t, int page, uint32_t dst, uint32_t full) {
+            if (lane == 0) bar_expect(full, L::kTileBytes);
+            __syncwarp();
+            if (lane < boxes) {
+                const int y = ps > kTile ? (t * kTile) & (ps - 1) : 0;
 #pragma unroll
-                    for (int h = 0; h < L::kHalves; ++h) tma_load(dst + h * L::kHalfBytes, map, 64 * h, y, x.head, page, full + 8 * stage);
+                for (int h = 0; h < L::kHalves; ++h) tma_load(dst + lane * box * 128 + h * L::kHalfBytes, map, 64 * h, y, x.head, page, full);
+            }
+            __syncwarp();
+        };
+        if (warp == 8) {
+            AttWalk walk(K, start);
+            uint32_t n = 0, q_n = 0;
+            const auto publish = [&](AttPiece &y, bool there) {
+                if (!there) y.t1 = 0;
+                bar_wait(piece_empty(piece_slot), piece_phase ^ 1u, gave_up);
+                if (lane == 0) {
+                    pieces[piece_slot] = y;
+                    bar_arrive(piece_full(piece_slot));
                 }
-                __syncwarp();
-                if (++stage == stages) { stage = 0; phase ^= 1u; }
-                page = next;
-                if (keys && t == x.t0) {   // (behind the first keys: a slot may not be free yet)
-                    const AttRows &r = x.shared ? P.shared : P.own;
-                    for (int i = 0; i < (x.two ? 2 : 1); ++i) {
-                        bar_wait(q_empty(q_slot), q_phase, gave_up);
+                if (++piece_slot == kPieces) { piece_slot = 0; piece_phase ^= 1u; }
+            };
+            bool there = walk.next(x);
+            publish(x, there);
+            while (there && *gave_up == 0) {
+                AttPiece y = {};
+                bool then = false;
+                int page = page_at(x.t0);
+                for (int t = x.t0; t < x.t1; ++t, ++n) {
+                    const int next = page_at(t + 1);
+                    bar_wait(k_empty(n % SK), (n / SK & 1u) ^ 1u, gave_up);
+                    bring(&maps.k, t, page, s_k + n % SK * L::kTileBytes, k_full(n % SK));
+                    page = next;
+                    if (t != x.t0) continue;
+                    // behind the first keys: the queries (a slot may not be free yet), and the piece after this one
+                    for (int i = 0; i < (x.two ? 2 : 1); ++i, ++q_n) {
+                        const uint32_t slot = q_n & 1u;
+                        bar_wait(q_empty(slot), (q_n / 2 & 1u) ^ 1u, gave_up);
                         if (lane == 0) {
+                            const AttRows &r = x.shared ? P.shared : P.own;
                             const AttTile o = tile_of(K, x.shared, 2 * x.block + i);
                             int z = o.node, w = x.b;
                             if (x.shared) {
                                 w = P.merged ? 0 : P.sequence.quot(o.node);
                                 z = o.node - w * c.nodes;
                             }
-                            bar_expect(q_full(q_slot), r.nodes * P.group.d * 2 * D);   // (what is out of range counts too)
+                            bar_expect(q_full(slot), r.nodes * P.group.d * 2 * D);   // (what is out of range counts too)
                             for (int h = 0; h < L::kHalves; ++h)
-                                tma_load(s_q + q_slot * L::kTileBytes + h * L::kHalfBytes, x.shared ? &maps.q_shared : &maps.q, 64 * h, x.head * P.group.d, z, w,
-                                         q_full(q_slot));
+                                tma_load(s_q + slot * L::kTileBytes + h * L::kHalfBytes, x.shared ? &maps.q_shared : &maps.q, 64 * h, x.head * P.group.d, z, w, q_full(slot));
                         }
                         __syncwarp();
-                        if (++q_slot == 2) { q_slot = 0; q_phase ^= 1u; }
                     }
-                }
-            }
-        }
-        // the rings' last arrivals come before the CTA ends
-        for (int s = 0; s < stages; ++s) {
-            bar_wait(empty + 8 * stage, phase, gave_up);
-            if (++stage == stages) { stage = 0; phase ^= 1u; }
-        }
-        for (int s = 0; s < 2 && keys; ++s) {
-            bar_wait(q_empty(q_slot), q_phase, gave_up);
-            if (++q_slot == 2) { q_slot = 0; q_phase ^= 1u; }
-        }
-    } else if (warp == 9) {
-        // ---- matrix instructions: one thread ---------------------------------------------------------
-        if (lane == 0) {
-            int ks = 0, vs = 0, q_slot = 0;
-            uint32_t k_phase = 0, v_phase = 0, q_phase = 0, p_phase = 0, free_phase = 1, clean_phase = 0;
-            constexpr uint32_t desc_s = mma_desc(kBf16, kTile, false), desc_o = mma_desc(kBf16, D, true);
-            const uint32_t k_op = operand(s_k, L::kHalfBytes), v_op = operand(s_v, L::kHalfBytes), q_op = operand(s_q, L::kHalfBytes);
-            const auto queries = [&]() {
-                bar_wait_one(q_full(q_slot), q_phase, gave_up);
-                const int s = q_slot;
-                if (++q_slot == 2) { q_slot = 0; q_phase ^= 1u; }
-                return s;
-            };
-            bool there = walk.next(x);
-            while (there) {
-                AttPiece y = {};
-                bool then = false;
-                // queries of both groups, or of one tile in whichever slot is next
-                const int q0 = queries(), q1 = x.two ? queries() : q0, ahead = x.two ? 1 : 2;
-                // Products of tile t, scores of tile t + ahead: each once in the code, which other warps push out of the instruction cache.
-                for (int t = x.t0 - ahead; t < x.t1; ++t) {
-                    const bool now = t >= x.t0, more = t + ahead < x.t1;
-                    if (now) {
-                        bar_wait_one(v_full(vs), v_phase, gave_up);
-                        if (x.masked(t)) {
-                            bar_arrive(v_here);
-                            if (t == x.t1 - 1) then = walk.next(y);   // (meanwhile)
-                            bar_wait_one(v_clean, clean_phase, gave_up);
-                            clean_phase ^= 1u;
-                        } else if (t == x.t1 - 1) then = walk.next(y);
-                        if (t == x.t0) {   // O of the piece before has been read by now or soon
-                            bar_wait_one(o_free, free_phase, gave_up);
-                            free_phase ^= 1u;
-                        }
-                    }
-                    if (more && (x.two || !now)) bar_wait_one(k_full(ks), k_phase, gave_up);
-                    const int g0 = x.two ? 0 : (t + ahead - x.t0) & 1, g1 = x.two ? 2 : g0 + 1;
-                    for (int g = g0; g < g1; ++g) {
-                        if (now) {   // O_g (+)= P_g V
-                            const uint32_t a = tm + L::kP + g * L::kPStep, b = v_op + vs * (L::kTileBytes >> 4), d = tm + L::kO + g * D;
-                            const bool add = t >= x.t0 + ahead;
-                            bar_wait_one(p_full(g), p_phase >> g & 1u, gave_up);
-                            p_phase ^= 1u << g;
-                            tmem_fence_after();
-#pragma unroll
-                            for (int k = 0; k < kTile / 16; ++k) mma_ts(d, a + 8 * k, b + k * (2048 >> 4), desc_o, add || k > 0);
-                            if (g == g1 - 1) mma_commit(v_empty(vs));
-                        }
-                        if (more) {   // S_g = Q K^T
-                            if (now && !x.two) bar_wait_one(k_full(ks), k_phase, gave_up);   // (the products first: these keys may still be on their way)
-                            const uint32_t a = q_op + (g ? q1 : q0) * (L::kTileBytes >> 4), b = k_op + ks * (L::kTileBytes >> 4), d = tm + L::kS + g * kTile;
-#pragma unroll
-                            for (int k = 0; k < D / 16; ++k) {
-                                const uint32_t off = ((k / 4) * L::kHalfBytes + (k % 4) * 32) >> 4;
-                                mma_ss(d, a + off, b + off, desc_s, k > 0);
-                            }
-                            mma_commit(s_full(g));
-                            if (g == g1 - 1) mma_commit(k_empty(ks));
-                        } else if (now) mma_commit(o_full(g));
-                    }
-                    if (now && ++vs == SV) { vs = 0; v_phase ^= 1u; }
-                    if (more && ++ks == SK) { ks = 0; k_phase ^= 1u; }
+                    then = walk.next(y);
+                    publish(y, then);
                 }
                 x = y;
                 there = then;
             }
-            bar_wait_one(o_free, free_phase, gave_up);
-        }
-        __syncwarp();
-    } else {
-        // ---- values behind the end, and those of tree nodes that are no numbers: zero -----------------------
-        int n0 = 0;   // tile among the CTA's, of the piece's first
-        uint32_t here_phase = 0;
-        for (; walk.next(x); n0 += x.t1 - x.t0) {
-            for (int t = max(x.t0, x.plain / kTile); t < x.t1; ++t) {
-                const unsigned n = n0 + t - x.t0, s = n % SV;
-                bar_wait(v_here, here_phase, gave_up);   // (asked for: the ring is neither before nor behind this place)
-                here_phase ^= 1u;
-                bar_wait(v_full(s), (n / SV) & 1u, gave_up);
-                constexpr int kVecs = D / 8;
-                constexpr uint32_t kExp = kBf16 ? 0x7f807f80u : 0x7c007c00u;   // all ones: no finite number
-                const int r0 = max(0, x.plain - t * kTile), r1 = min(kTile, x.keys - t * kTile);
-                uint8_t *const v = smem + (2 + SK + s) * L::kTileBytes;
-                const auto place = [&](int i) { return reinterpret_cast<uint4 *>(v + (i % kVecs / 8) * L::kHalfBytes + (i / kVecs) * 128 + (i % 8) * 16); };
-                for (int i = lane + r1 * kVecs; i < kTile * kVecs; i += 32) *place(i) = make_uint4(0, 0, 0, 0);
-                uint32_t most = 0;   // of the magnitudes, as numbers of 15 bits
-                for (int i0 = r0 * kVecs; i0 < r1 * kVecs; i0 += 256) {
-                    uint4 u[8];
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) u[j] = *place(min(i0 + 32 * j + lane, r1 * kVecs - 1));
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        most = __vimax3_u16x2(most, u[j].x & 0x7fff7fffu, u[j].y & 0x7fff7fffu);
-                        most = __vimax3_u16x2(most, u[j].z & 0x7fff7fffu, u[j].w & 0x7fff7fffu);
-                    }
+            // the last arrivals come before the CTA ends
+            for (int i = 0; i < SK; ++i, ++n) bar_wait(k_empty(n % SK), (n / SK & 1u) ^ 1u, gave_up);
+            for (int i = 0; i < 2; ++i, ++q_n) bar_wait(q_empty(q_n & 1u), (q_n / 2 & 1u) ^ 1u, gave_up);
+        } else {
+            uint32_t n = 0;
+            while (next_piece(x)) {
+                int page = page_at(x.t0);
+                for (int t = x.t0; t < x.t1; ++t, ++n) {
+                    const int next = page_at(t + 1);
+                    bar_wait(v_empty(n % SV), (n / SV & 1u) ^ 1u, gave_up);
+                    bring(&maps.v, t, page, s_v + n % SV * L::kTileBytes, v_full(n % SV));
+                    page = next;
                 }
-                if (__any_sync(kFull, (most & 0xffffu) >= (kExp & 0xffffu) || most >> 16 >= kExp >> 16)) {
-                    for (int i = lane + r0 * kVecs; i < r1 * kVecs; i += 32) {
-                        uint4 u = *place(i);
-                        uint32_t *w = &u.x;
-                        for (int k = 0; k < 4; ++k) {
-                            if ((w[k] & kExp & 0xffffu) == (kExp & 0xffffu)) w[k] &= 0xffff0000u;
-                            if ((w[k] & kExp & 0xffff0000u) == (kExp & 0xffff0000u)) w[k] &= 0xffffu;
-                        }
-                        *place(i) = u;
-                    }
-                    *static_cast<volatile int *>(&bad_values) = 1;   // (from here on the CTA looks for such nodes)
-                }
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                __threadfence_block();
-                __syncwarp();
-                if (lane == 0) bar_arrive(v_clean);
             }
+            for (int i = 0; i < SV; ++i, ++n) bar_wait(v_empty(n % SV), (n / SV & 1u) ^ 1u, gave_up);
         }
     }
     tmem_fence_before();
@@ -795,24 +875,48 @@ __global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(const __gr
     for (int row = chunk * kJoinRows + (tid >> 5); row < min(rows, (chunk + 1) * kJoinRows); row += kJoinThreads / 32) {
         const int in = P.group.quot(row), n = t.node + in, h = hk * P.group.d + (row - in * P.group.d);
         float ref = neg_inf(), sum = 0.f, o[E] = {};
-        // the pieces of CTAs i0..i1 of a block whose costs begin at `at` (one whose run has no tile of it left nothing); `row0`: the first
-        // row of CTA 0's tile, `step`: rows from one CTA's to the next one's
+        // The pieces of CTAs i0..i1 of a block whose costs begin at `at` (one whose run has no tile of it left nothing), a lane for each;
+        // `row0`: the first row of CTA 0's tile, `step`: rows from one CTA's to the next one's.
         const auto add = [&](int at, int n_tiles, int i0, int i1, int64_t row0, int step, int rows_of, int r) {
-            for (int i = i0; i <= i1; ++i) {
-                const int t0 = tiles_before(split_first(i, all, P.grid) - at, n_tiles), t1 = tiles_before(split_first(i + 1, all, P.grid) - at, n_tiles);
-                if (t1 <= t0) continue;
-                const int64_t first = row0 + int64_t(i) * step;
-                const float2 ml = P.ml[first + r];
-                const int col = lane * E;
-                const float *src = P.o + first * D + (int64_t(col / 32) * rows_of + r) * 32 + ((col % 32 / 4) ^ (r & 7)) * 4 + col % 4;
-                float z[E];
-                if (E == 4) { const float4 v = *reinterpret_cast<const float4 *>(src); z[0] = v.x; z[1] = v.y; z[E - 2] = v.z; z[E - 1] = v.w; }
-                else { const float2 v = *reinterpret_cast<const float2 *>(src); z[0] = v.x; z[1] = v.y; }
-                const float now = fmaxf(ref, ml.x), m = now == neg_inf() ? 0.f : now, f0 = ex2(ref - m), f1 = ex2(ml.x - m);
-                sum = sum * f0 + ml.y * f1;
+            const int col = lane * E;
+            const float *src = P.o + row0 * D + (int64_t(col / 32) * rows_of + r) * 32 + ((col % 32 / 4) ^ (r & 7)) * 4 + col % 4;
+            for (; i0 <= i1; i0 += 32) {
+                const int i = i0 + lane;
+                const bool piece = i <= i1 && tiles_before(split_first(i + 1, all, P.grid) - at, n_tiles) > tiles_before(split_first(i, all, P.grid) - at, n_tiles);
+                const float2 ml = piece ? P.ml[row0 + int64_t(i) * step + r] : make_float2(neg_inf(), 0.f);
+                float now = ml.x;
+#pragma unroll
+                for (int x = 16; x > 0; x >>= 1) now = fmaxf(now, __shfl_xor_sync(kFull, now, x));
+                now = fmaxf(now, ref);
+                const float m = now == neg_inf() ? 0.f : now, f0 = ex2(ref - m), f = ex2(ml.x - m);   // (a reference that is no number: so is the sum)
+                float l = f * ml.y;
+#pragma unroll
+                for (int x = 16; x > 0; x >>= 1) l += __shfl_xor_sync(kFull, l, x);
+                sum = sum * f0 + l;
                 ref = now;
 #pragma unroll
-                for (int k = 0; k < E; ++k) o[k] = o[k] * f0 + z[k] * f1;
+                for (int k = 0; k < E; ++k) o[k] *= f0;
+                unsigned left = __ballot_sync(kFull, piece);
+                while (left) {   // four pieces' loads at once
+                    float z[4][E], w[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int at_lane = left ? __ffs(left) - 1 : 0;
+                        w[j] = left ? __shfl_sync(kFull, f, at_lane) : 0.f;
+                        const float *p = src + int64_t(i0 + at_lane) * step * D;
+#pragma unroll
+                        for (int k = 0; k < E; ++k) z[j][k] = 0.f;
+                        if (left) {
+                            if (E == 4) { const float4 v = *reinterpret_cast<const float4 *>(p); z[j][0] = v.x; z[j][1] = v.y; z[j][E - 2] = v.z; z[j][E - 1] = v.w; }
+                            else { const float2 v = *reinterpret_cast<const float2 *>(p); z[j][0] = v.x; z[j][1] = v.y; }
+                        }
+                        left &= left - 1;
+                    }
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+#pragma unroll
+                        for (int k = 0; k < E; ++k) o[k] = fmaf(z[j][k], w[j], o[k]);
+                }
             }
         };
         if (P.shared_tiles) {
