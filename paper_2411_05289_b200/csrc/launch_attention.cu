@@ -3,7 +3,6 @@
 
 #include "spechub_attention.cuh"
 #include "spechub_cache_launch.h"
-#include "spechub_shapes.h"
 
 namespace spechub {
 
@@ -102,15 +101,21 @@ bool plan_of(const CacheArgs &c, const HeadsPtr &q, int64_t shared_len, uint8_t 
     // (the size goes by the shape alone, whichever strides the queries have)
     const auto shared_rows = [&](const AttRows &r) { return shared_len ? (static_cast<int64_t>(c.kv_heads) * r.blocks + kSms) * slot(r) : 0; };
     const int64_t room = own_rows + (shared_rows(merged) > shared_rows(apart) ? shared_rows(merged) : shared_rows(apart));
+    // four rows for each warp that joins, or one where that leaves SMs idle
+    p->join_rows = shared_len && own_items * c.nodes * group >= 4 * 32 * kSms ? 4 : 1;
     size_t at = 0;
     p->before = reinterpret_cast<int *>(base);
     at += up(sizeof(int) * (static_cast<size_t>(c.batch) + 1));
+    p->first = reinterpret_cast<int *>(base + at);
+    at += up(sizeof(int) * (kSms + 1));
     p->error = reinterpret_cast<int *>(base + at);
     at += up(sizeof(int) * kSms);
+    p->begin = reinterpret_cast<int4 *>(base + at);
+    at += up(sizeof(int4) * kSms);
     p->ml = reinterpret_cast<float2 *>(base + at);
     at += up(sizeof(float2) * static_cast<size_t>(rows));
     p->o = reinterpret_cast<float *>(base + at);
-    *bytes = up(sizeof(int) * (static_cast<size_t>(c.batch) + 1)) + up(sizeof(int) * kSms) + up(sizeof(float2) * static_cast<size_t>(room)) +
+    *bytes = up(sizeof(int) * (static_cast<size_t>(c.batch) + 1)) + up(sizeof(int) * (kSms + 1)) + up(sizeof(int) * kSms) + up(sizeof(int4) * kSms) + up(sizeof(float2) * static_cast<size_t>(room)) +
              up(sizeof(float) * static_cast<size_t>(room) * c.head_dim);
     return true;
 }
@@ -133,9 +138,10 @@ int launch_type(const AttKernelArgs &k, const AttMaps &maps, cudaStream_t s) {
     const int lrc = launch_grid(attention_kernel<T, D>, k.p.grid, kAttThreads, AttShape<D>::kSmem, 1, s, k, maps);
     if (lrc != SPECHUB_OK) return lrc;
     const AttRows &r = k.p.own;
-    const int64_t grid = static_cast<int64_t>(k.a.c.batch) * k.a.c.kv_heads * r.blocks * r.slot_tiles * ((r.slot_rows + kJoinRows - 1) / kJoinRows) +
-                         (k.a.c.status ? k.a.c.batch : 0);
-    if (grid > 0x7fffffffLL) return SPECHUB_ERR_SHAPE;
+    const int64_t blocks = k.p.shared_tiles ? static_cast<int64_t>(k.a.c.batch) * k.a.c.kv_heads * r.blocks : k.p.grid;
+    const int64_t tasks = blocks * r.slot_tiles * ((r.slot_rows + k.p.join_rows - 1) / k.p.join_rows), per = kJoinThreads / 32;
+    const int64_t grid = (tasks + per - 1) / per + (k.a.c.status ? k.a.c.batch : 0);
+    if (tasks > 0x7fffffffLL) return SPECHUB_ERR_SHAPE;
     return launch_grid(attention_join_kernel<T, D>, static_cast<unsigned>(grid), kJoinThreads, 0, 1, s, k);
 }
 

@@ -30,6 +30,7 @@
 #pragma once
 
 #include "spechub_pages.cuh"
+#include "spechub_shapes.h"
 #include "spechub_tmem.cuh"
 #include "spechub_umma.cuh"
 
@@ -90,7 +91,10 @@ struct AttPlan {
     bool merged;                  // the batch's nodes are one axis of the queries' shared tensor map, else sequences are its last
     FastDiv group, sequence;      // query heads per cache head; nodes per sequence
     int *before;                  // [batch + 1] cost of the own blocks before sequence b
+    int *first;                   // [grid + 1] where each CTA's costs begin, and the sum of all
     int *error;                   // [grid]
+    int4 *begin;                  // [grid] where each CTA's first piece is: sequence, head, block, first tile (0 also if it has none)
+    int join_rows;                // rows of a tile that a warp joins
     float2 *ml;                   // (reference, sum) of every row of every slot
     float *o;                     // of every tile of a slot [head_dim / 32][rows][32], not divided by the sum; vectors of four swapped (row & 7)
 };
@@ -118,10 +122,6 @@ __device__ __forceinline__ int split_first(int cta, int all, int grid) {
     const unsigned q = static_cast<unsigned>(all) / grid, r = static_cast<unsigned>(all) - q * grid;
     return cta * q + (cta * r + grid - 1) / grid;
 }
-__device__ __forceinline__ int split_cta(int cost, int all, int grid) {
-    return static_cast<int>(static_cast<unsigned long long>(static_cast<unsigned>(cost)) * grid / static_cast<unsigned>(all));
-}
-
 // Consecutive tiles of keys for one block of rows.
 struct AttPiece {
     bool shared, two;      // two: the block has two tiles of rows
@@ -390,7 +390,12 @@ __global__ void __launch_bounds__(kAttThreads, 1) attention_kernel(const __grid_
             const int in_b = (from - before) / last;
             start = AttStart{from, to, before + in_b * last, false, b, in_b / P.own.blocks, in_b % P.own.blocks};
         }
-        if (blockIdx.x == 0 && b0 < b1) {   // for the kernel that joins
+        // for the kernel that joins
+        if (tid == 0) {
+            P.first[blockIdx.x] = from;
+            if (blockIdx.x == gridDim.x - 1) P.first[gridDim.x] = all;
+        }
+        if (blockIdx.x == 0 && b0 < b1) {
             before = upto - mine;
             for (int b = b0; b < b1; ++b) {
                 P.before[b] = before;
@@ -689,9 +694,9 @@ __global__ void __launch_bounds__(kAttThreads, 1) attention_kernel(const __grid_
                     if (now) {   // O (+)= P V
                         const uint32_t b = v_op + v_slot * (L::kTileBytes >> 4);
                         const bool add = i > first;
+                        my_turn();
                         bar_wait_one(p_full(g), p_phase, gave_up);
                         p_phase ^= 1u;
-                        my_turn();
                         tmem_fence_after();
 #pragma unroll
                         for (int k = 0; k < kTile / 16; ++k) mma_ts(d_o, a_p + 8 * k, b + k * (2048 >> 4), desc_o, add || k > 0);
@@ -763,6 +768,7 @@ __global__ void __launch_bounds__(kAttThreads, 1) attention_kernel(const __grid_
                 if (++piece_slot == kPieces) { piece_slot = 0; piece_phase ^= 1u; }
             };
             bool there = walk.next(x);
+            if (lane == 0) P.begin[blockIdx.x] = make_int4(x.b, x.head, x.block, there && !x.shared ? x.t0 : 0);
             publish(x, there);
             while (there && *gave_up == 0) {
                 AttPiece y = {};
@@ -826,10 +832,11 @@ __global__ void __launch_bounds__(kAttThreads, 1) attention_kernel(const __grid_
     if (warp == 9) tmem_dealloc(tm, 512);
 }
 
-constexpr int kJoinThreads = 256, kJoinRows = 32;
+constexpr int kJoinThreads = 256, kJoinAtOnce = 4;
 
-// Joins the pieces of every block that has more than one, kJoinRows rows of a tile per CTA, a warp per row; and finds bad pages (the first
-// `batch` CTAs, if wanted).
+// Joins the pieces of the blocks that have more than one, P.join_rows rows of a tile per warp; and finds bad pages (the first `batch` CTAs,
+// if wanted).  Where there is a prefix that is all blocks; where there is none, it is those that some CTA begins in the middle of,
+// found from that CTA.  What bounds it is the chain of loads: where the pieces are, then their rows, kJoinAtOnce at a time.
 template <class T, int D>
 __global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(const __grid_constant__ AttKernelArgs K) {
     constexpr int E = D / 32;
@@ -838,10 +845,10 @@ __global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(const __gr
     const CacheArgs &c = A.c;
     const AttPlan &P = K.p;
     const int tid = threadIdx.x, lane = tid & 31;
-    int block = blockIdx.x;
+    int task = blockIdx.x;
     if (c.status) {
-        if (block < c.batch) {
-            const int b = block, ps = 1 << c.page_shift, len = c.lens[b];
+        if (task < c.batch) {
+            const int b = task, ps = 1 << c.page_shift, len = c.lens[b];
             bool bad = false, error = false;
             if (len >= 0) {
                 const int64_t need = (static_cast<int64_t>(len) + c.nodes + ps - 1) >> c.page_shift;
@@ -857,83 +864,110 @@ __global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(const __gr
             if (tid == 0) c.status[b] = (bad ? SPECHUB_ST_PAGE : 0u) | (error ? SPECHUB_ST_INTERNAL : 0u);
             return;
         }
-        block -= c.batch;
+        task -= c.batch;
     }
-    const int chunks = (P.own.slot_rows + kJoinRows - 1) / kJoinRows, chunk = block % chunks;   // of a tile of rows
-    block /= chunks;
-    const int tb = block % P.own.slot_tiles, item = block / P.own.slot_tiles, per_b = c.kv_heads * P.own.blocks, b = item / per_b, in_b = item - b * per_b;
-    const int len = c.lens[b];
-    if (len < 0) return;
-    const int tiles = own_tiles(c, len), each = block_cost(tiles), all = P.before[c.batch];
-    const int own0 = P.before[b] + in_b * each;                       // the block's costs begin here, its tiles' kBlockCost later
-    const int c0 = split_cta(own0 + kBlockCost, all, P.grid), c1 = split_cta(own0 + each - 1, all, P.grid);
-    if (P.shared_tiles == 0 && tiles_before(split_first(c0 + 1, all, P.grid) - own0, tiles) == tiles) return;   // finished in place
-    const int hk = in_b / P.own.blocks, tile = 2 * (in_b - hk * P.own.blocks) + tb;
-    if (tile >= P.own.tiles) return;
+    task = task * (kJoinThreads / 32) + (tid >> 5);
+    const int chunks = (P.own.slot_rows + P.join_rows - 1) / P.join_rows, chunk = task % chunks;   // of a tile of rows
+    task /= chunks;
+    const int tb = task % P.own.slot_tiles;
+    task /= P.own.slot_tiles;
+    int b, hk, block;
+    if (P.shared_tiles) {
+        const int per_b = c.kv_heads * P.own.blocks;
+        b = task / per_b;
+        hk = (task - b * per_b) / P.own.blocks;
+        block = task - b * per_b - hk * P.own.blocks;
+        if (b >= c.batch) return;
+    } else {
+        if (task >= P.grid) return;
+        const int4 at = P.begin[task];
+        if (at.w == 0) return;
+        b = at.x; hk = at.y; block = at.z;
+    }
+    const int tile = 2 * block + tb, len = c.lens[b];
+    if (len < 0 || tile >= P.own.tiles) return;
     const AttTile t = tile_of(K, false, tile);
-    const int rows = t.count * P.group.d;
-    for (int row = chunk * kJoinRows + (tid >> 5); row < min(rows, (chunk + 1) * kJoinRows); row += kJoinThreads / 32) {
-        const int in = P.group.quot(row), n = t.node + in, h = hk * P.group.d + (row - in * P.group.d);
+    const int row0 = chunk * P.join_rows, row1 = min(t.count * static_cast<int>(P.group.d), row0 + P.join_rows);
+    if (row0 >= row1) return;
+    const int tiles = own_tiles(c, len), own0 = P.before[b] + (hk * P.own.blocks + block) * block_cost(tiles), all = P.first[P.grid];
+    if (!P.shared_tiles) {   // of the CTAs that begin within the block, the first one's task is this
+        const int from = P.begin[task].w;
+        int i = task - 1, before = 0;
+        while (i > 0 && (before = tiles_before(P.first[i] - own0, tiles)) == from) --i;   // (a run can be too short for a tile)
+        if (i > 0 && before > 0) return;
+    }
+    const int item = (b * c.kv_heads + hk) * P.own.blocks + block;
+    const int step = P.own.slot_tiles * P.own.slot_rows, s_step = P.shared.slot_tiles * P.shared.slot_rows;
+    const int64_t own_row = P.shared_slots * s_step + static_cast<int64_t>(item) * step + tb * P.own.slot_rows;
+    // the first CTA whose run may have tiles of a block whose costs begin at `at`
+    const auto first_cta = [&](int at) {
+        int i = min(P.grid - 1, at / max(1, all / P.grid));   // (not before the one that has cost `at`, and hardly behind it)
+        while (i > 0 && P.first[i] > at) --i;
+        return i;
+    };
+    const int own_cta = first_cta(own0);
+    for (int row = row0; row < row1; ++row) {
+        const int in = P.group.quot(row), n = t.node + in, h = hk * P.group.d + (row - in * P.group.d), col = lane * E;
         float ref = neg_inf(), sum = 0.f, o[E] = {};
-        // The pieces of CTAs i0..i1 of a block whose costs begin at `at` (one whose run has no tile of it left nothing), a lane for each;
-        // `row0`: the first row of CTA 0's tile, `step`: rows from one CTA's to the next one's.
-        const auto add = [&](int at, int n_tiles, int i0, int i1, int64_t row0, int step, int rows_of, int r) {
-            const int col = lane * E;
-            const float *src = P.o + row0 * D + (int64_t(col / 32) * rows_of + r) * 32 + ((col % 32 / 4) ^ (r & 7)) * 4 + col % 4;
-            for (; i0 <= i1; i0 += 32) {
-                const int i = i0 + lane;
-                const bool piece = i <= i1 && tiles_before(split_first(i + 1, all, P.grid) - at, n_tiles) > tiles_before(split_first(i, all, P.grid) - at, n_tiles);
-                const float2 ml = piece ? P.ml[row0 + int64_t(i) * step + r] : make_float2(neg_inf(), 0.f);
-                float now = ml.x;
-#pragma unroll
-                for (int x = 16; x > 0; x >>= 1) now = fmaxf(now, __shfl_xor_sync(kFull, now, x));
-                now = fmaxf(now, ref);
-                const float m = now == neg_inf() ? 0.f : now, f0 = ex2(ref - m), f = ex2(ml.x - m);   // (a reference that is no number: so is the sum)
-                float l = f * ml.y;
-#pragma unroll
-                for (int x = 16; x > 0; x >>= 1) l += __shfl_xor_sync(kFull, l, x);
-                sum = sum * f0 + l;
-                ref = now;
-#pragma unroll
-                for (int k = 0; k < E; ++k) o[k] *= f0;
+        // The pieces of a block: of the CTAs from `cta`, whose first rows in the workspace are row_0 + i * by; a lane looks at each.
+        const auto add = [&](int at, int n_tiles, int cta, int64_t row_0, int by, int rows_of, int r) {
+            const float *src = P.o + row_0 * D + ((col / 32) * rows_of + r) * 32 + ((col % 32 / 4) ^ (r & 7)) * 4 + col % 4;
+            const int end = at + block_cost(n_tiles);
+            for (; cta < P.grid; cta += 32) {
+                const int i = cta + lane, from = i <= P.grid ? P.first[i] : 0x7fffffff, to = i < P.grid ? P.first[i + 1] : 0x7fffffff;
+                const bool piece = i < P.grid && from < end && tiles_before(to - at, n_tiles) > tiles_before(from - at, n_tiles);
                 unsigned left = __ballot_sync(kFull, piece);
-                while (left) {   // four pieces' loads at once
-                    float z[4][E], w[4];
+                while (left) {
+                    float z[kJoinAtOnce][E];
+                    float2 ml[kJoinAtOnce];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const int at_lane = left ? __ffs(left) - 1 : 0;
-                        w[j] = left ? __shfl_sync(kFull, f, at_lane) : 0.f;
-                        const float *p = src + int64_t(i0 + at_lane) * step * D;
+                    for (int j = 0; j < kJoinAtOnce; ++j) {
+                        ml[j] = make_float2(neg_inf(), 0.f);
 #pragma unroll
                         for (int k = 0; k < E; ++k) z[j][k] = 0.f;
                         if (left) {
-                            if (E == 4) { const float4 v = *reinterpret_cast<const float4 *>(p); z[j][0] = v.x; z[j][1] = v.y; z[j][E - 2] = v.z; z[j][E - 1] = v.w; }
-                            else { const float2 v = *reinterpret_cast<const float2 *>(p); z[j][0] = v.x; z[j][1] = v.y; }
+                            const int64_t off = static_cast<int64_t>(cta + __ffs(left) - 1) * by;
+                            ml[j] = P.ml[row_0 + off + r];
+                            if (E == 4) { const float4 v = *reinterpret_cast<const float4 *>(src + off * D); z[j][0] = v.x; z[j][1] = v.y; z[j][E - 2] = v.z; z[j][E - 1] = v.w; }
+                            else { const float2 v = *reinterpret_cast<const float2 *>(src + off * D); z[j][0] = v.x; z[j][1] = v.y; }
+                            left &= left - 1;
                         }
-                        left &= left - 1;
                     }
+                    float now = ref;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
+                    for (int j = 0; j < kJoinAtOnce; ++j) now = fmaxf(now, ml[j].x);
+                    const float m = now == neg_inf() ? 0.f : now, f0 = ex2(ref - m);
+                    sum *= f0;
 #pragma unroll
-                        for (int k = 0; k < E; ++k) o[k] = fmaf(z[j][k], w[j], o[k]);
+                    for (int k = 0; k < E; ++k) o[k] *= f0;
+#pragma unroll
+                    for (int j = 0; j < kJoinAtOnce; ++j) {
+                        const float f = ex2(ml[j].x - m);
+                        sum = fmaf(ml[j].y, f, sum);
+#pragma unroll
+                        for (int k = 0; k < E; ++k) o[k] = fmaf(z[j][k], f, o[k]);
+                    }
+                    ref = now;
                 }
+                if (__any_sync(kFull, from >= end)) break;
             }
         };
-        if (P.shared_tiles) {
+        if (P.shared_tiles) {   // the row's place among those of the whole batch
             const AttRows &r = P.shared;
             const int node = b * c.nodes + n, period = r.by_period.quot(node), in_p = node - period * r.period, part = r.by_nodes.quot(in_p);
             const int s_tile = period * r.parts + part, s_row = (in_p - part * r.nodes) * P.group.d + (row - in * P.group.d);
-            const int s_item = hk * r.blocks + s_tile / 2, s_each = block_cost(P.shared_tiles), at = s_item * s_each, step = r.slot_tiles * r.slot_rows;
-            add(at, P.shared_tiles, split_cta(at + kBlockCost, all, P.grid), split_cta(at + s_each - 1, all, P.grid),
-                int64_t(s_item) * step + s_tile % 2 * r.slot_rows, step, r.slot_rows, s_row);
+            const int s_item = hk * r.blocks + s_tile / 2, at = s_item * block_cost(P.shared_tiles);
+            add(at, P.shared_tiles, first_cta(at), static_cast<int64_t>(s_item) * s_step + s_tile % 2 * r.slot_rows, s_step, r.slot_rows, s_row);
         }
-        const int step = P.own.slot_tiles * P.own.slot_rows;
-        add(own0, tiles, c0, c1, P.shared_slots * P.shared.slot_tiles * P.shared.slot_rows + int64_t(item) * step + tb * P.own.slot_rows, step, P.own.slot_rows, row);
+        add(own0, tiles, own_cta, own_row, step, P.own.slot_rows, row);
         const bool none = sum == 0.f;
         const float inv = none ? 0.f : 1.f / sum;
-        T *dst = static_cast<T *>(A.out.data) + b * A.out.seq + n * A.out.node + h * A.out.head + lane * E;
+        T *dst = static_cast<T *>(A.out.data) + b * A.out.seq + n * A.out.node + h * A.out.head + col;
+        uint32_t w[E / 2];
 #pragma unroll
-        for (int i = 0; i < E; i += 2) *reinterpret_cast<uint32_t *>(dst + i) = pack2<T>(o[i] * inv, o[i + 1] * inv);
+        for (int k = 0; k < E; k += 2) w[k / 2] = pack2<T>(o[k] * inv, o[k + 1] * inv);
+        if (E == 4) *reinterpret_cast<uint2 *>(dst) = make_uint2(w[0], w[E / 2 - 1]);
+        else *reinterpret_cast<uint32_t *>(dst) = w[0];
         if (A.lse && lane == 0) A.lse[(int64_t(b) * c.nodes + n) * c.heads + h] = none ? neg_inf() : (ref + log2f(sum)) * 0.6931471805599453f;
     }
 }
