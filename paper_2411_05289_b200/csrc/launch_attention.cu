@@ -52,7 +52,7 @@ int heads_map(int dtype, const HeadsPtr &x, const CacheArgs &c, int64_t nodes_al
                       {x.head, x.node, x.seq}, {64, static_cast<cuuint32_t>(c.heads / c.kv_heads), static_cast<cuuint32_t>(nodes), static_cast<cuuint32_t>(sequences)}, map);
 }
 
-AttRows rows_of(int64_t group, int64_t nodes, int64_t period, int64_t all) {
+AttRows rows_of(int head_dim, int64_t group, int64_t nodes, int64_t period, int64_t all) {
     AttRows r = {};
     r.nodes = static_cast<int>(nodes);
     r.parts = static_cast<int>((period + nodes - 1) / nodes);
@@ -60,6 +60,7 @@ AttRows rows_of(int64_t group, int64_t nodes, int64_t period, int64_t all) {
     r.tiles = static_cast<int>((all + period - 1) / period * r.parts);
     r.blocks = (r.tiles + 1) / 2;
     r.slot_tiles = r.tiles > 1 ? 2 : 1;
+    r.tile_cost = tile_cost(head_dim, r.tiles > 1);
     r.slot_rows = static_cast<int>(nodes * group);
     r.by_nodes = FastDiv::of(static_cast<uint32_t>(nodes));
     r.by_period = FastDiv::of(static_cast<uint32_t>(period));
@@ -73,22 +74,25 @@ size_t up(size_t n) { return (n + 255) & ~size_t(255); }
 bool plan_of(const CacheArgs &c, const HeadsPtr &q, int64_t shared_len, uint8_t *base, AttPlan *p, size_t *bytes) {
     const int64_t group = c.heads / c.kv_heads, most_nodes = kTile / group, all = static_cast<int64_t>(c.batch) * c.nodes;
     const int64_t own_nodes = c.nodes < most_nodes ? c.nodes : most_nodes;
-    p->own = rows_of(group, own_nodes, c.nodes, c.nodes);
+    p->own = rows_of(c.head_dim, group, own_nodes, c.nodes, c.nodes);
     // Rows of the whole batch: tiles go on from one sequence to the next where one stride leads through all nodes; otherwise they hold as
     // many whole sequences as fit, or parts of one.  (The workspace has room for either.)
     p->merged = c.batch == 1 || c.nodes == 1 || q.seq == q.node * c.nodes;
     const int64_t merged_nodes = all < most_nodes ? all : most_nodes;
     const int64_t whole = most_nodes / c.nodes < c.batch ? most_nodes / c.nodes : c.batch;   // sequences in a tile
-    const AttRows merged = rows_of(group, merged_nodes, merged_nodes, all);
-    const AttRows apart = whole >= 1 ? rows_of(group, whole * c.nodes, whole * c.nodes, all) : rows_of(group, own_nodes, c.nodes, all);
+    const AttRows merged = rows_of(c.head_dim, group, merged_nodes, merged_nodes, all);
+    const AttRows apart = whole >= 1 ? rows_of(c.head_dim, group, whole * c.nodes, whole * c.nodes, all) : rows_of(c.head_dim, group, own_nodes, c.nodes, all);
     p->shared = p->merged ? merged : apart;
     p->shared_tiles = static_cast<int>((shared_len + kTile - 1) / kTile);
     const int64_t own_items = static_cast<int64_t>(c.batch) * c.kv_heads * p->own.blocks;
     const int64_t shared_items = shared_len ? static_cast<int64_t>(c.kv_heads) * p->shared.blocks : 0;
     const int64_t own_tiles = ((static_cast<int64_t>(c.table_width) << c.page_shift) + kTile - 1) / kTile;   // of a sequence, at most
-    const double most = double(shared_items) * (kBlockCost + double(kTileCost) * p->shared_tiles) + double(own_items) * (kBlockCost + double(kTileCost) * own_tiles);
+    // (at most every tile of keys is masked)
+    const auto cost = [](const AttRows &r, double tiles) { return kBlockCost + tiles * (r.tile_cost + kMaskedCost); };
+    const double most = double(shared_items) * cost(p->shared, p->shared_tiles) + double(own_items) * cost(p->own, double(own_tiles));
     if (most > 2.0e9) return false;
-    p->shared_cost = static_cast<int>(shared_items * (kBlockCost + static_cast<int64_t>(kTileCost) * p->shared_tiles));
+    const int64_t masked = p->shared_tiles - shared_len / kTile;
+    p->shared_cost = static_cast<int>(shared_items * (kBlockCost + masked * kMaskedCost + static_cast<int64_t>(p->shared.tile_cost) * p->shared_tiles));
     p->group = FastDiv::of(static_cast<uint32_t>(group));
     p->sequence = FastDiv::of(static_cast<uint32_t>(c.nodes));
     // as many CTAs as there can be tiles, at most one per SM

@@ -72,14 +72,19 @@ struct FastDiv {
     __device__ uint32_t quot(uint32_t x) const { return (__umulhi(m, x) + x) >> s; }
 };
 
-// What the host knows of the work.  A block of `tiles` tiles costs kBlockCost + tiles * (shared_cost or own_cost), and the CTAs share
-// the sum of the costs evenly.
-constexpr int kBlockCost = 6, kTileCost = 4;
+// What the host knows of the work.  A block of rows costs kBlockCost, kMaskedCost for every tile of keys that not all of its rows see
+// whole, and AttRows::tile_cost for every tile; the CTAs share the sum of the costs evenly.
+//   Measured, in units of 0.4 us: a tile of one tile of rows is what its bytes take (1.5 us; half of that for heads of 64), with two it is
+// their exponentials (2.4 us); the turnover between pieces 3 us; a masked tile 3 us more.  (Without the difference: the prompt's chunk
+// 198 us and not 149, 64 sequences of 31 nodes 153 and not 137.)
+constexpr int kBlockCost = 8, kMaskedCost = 8;
+constexpr int tile_cost(int head_dim, bool two) { return two ? 6 : head_dim == 64 ? 3 : 4; }
 
 // Rows in tiles.  A tile is `nodes` nodes (all query heads of a cache head), at most 128 rows.  `parts` tiles follow each other within
 // `period` nodes, then the next period begins: the nodes of one sequence, or (parts = 1, period = nodes) of the batch as it goes on.
 struct AttRows {
     int nodes, parts, period, tiles, blocks;   // blocks of two tiles, per cache head
+    int tile_cost;                             // of a tile of keys
     int slot_tiles, slot_rows;                 // of a block in the workspace: tiles, and rows of each
     FastDiv by_nodes, by_period, by_parts;
 };
@@ -112,10 +117,15 @@ __device__ __forceinline__ int own_end(const CacheArgs &c, int len) {   // keys 
 __device__ __forceinline__ int own_tiles(const CacheArgs &c, int len) {
     return len < 0 ? 0 : static_cast<int>((static_cast<unsigned>(own_end(c, len)) + kTile - 1) / kTile);
 }
-__device__ __forceinline__ int block_cost(int tiles) { return tiles ? kBlockCost + tiles * kTileCost : 0; }
-// tiles of a block that lie before `cost`, counted from the block's start
-__device__ __forceinline__ int tiles_before(int cost, int tiles) {
-    return min(tiles, max(0, (cost - kBlockCost + kTileCost - 1) / kTileCost));
+// What precedes a block's tiles in the costs; the block's cost; and tiles that lie before `cost`, counted from the block's start.
+__device__ __forceinline__ int head_cost(int plain, int tiles) { return kBlockCost + (tiles - plain / kTile) * kMaskedCost; }
+__device__ __forceinline__ int block_cost(int head, int tiles, int tile_cost) { return tiles ? head + tiles * tile_cost : 0; }
+__device__ __forceinline__ int tiles_before(int cost, int head, int tiles, int tile_cost) {
+    return min(tiles, max(0, cost - head + tile_cost - 1) / tile_cost);
+}
+__device__ __forceinline__ int own_cost(const CacheArgs &c, const AttRows &r, int len) {
+    const int tiles = own_tiles(c, len);
+    return tiles ? block_cost(head_cost(min(len, own_end(c, len)), tiles), tiles, r.tile_cost) : 0;
 }
 // Blocks are numbered: all of the shared prefix, then sequence by sequence.  Of the whole cost `all`, CTA i takes [first(i), first(i + 1)).
 __device__ __forceinline__ int split_first(int cta, int all, int grid) {
@@ -163,13 +173,14 @@ struct AttWalk {
             x.block = block;
             x.tiles = tiles;
             x.two = 2 * block + 1 < r.tiles;
-            x.t0 = from > at ? tiles_before(from - at, tiles) : 0;
-            x.t1 = tiles_before(to - at, tiles);
             x.b = shared ? 0 : b;
             x.item = (x.b * c.kv_heads + head) * r.blocks + block;
             x.keys = shared ? shared_len : own_end(c, len);
             x.plain = shared ? shared_len : min(len, x.keys);
-            at += block_cost(tiles);
+            const int ahead = head_cost(x.plain, tiles);
+            x.t0 = from > at ? tiles_before(from - at, ahead, tiles, r.tile_cost) : 0;
+            x.t1 = tiles_before(to - at, ahead, tiles, r.tile_cost);
+            at += block_cost(ahead, tiles, r.tile_cost);
             if (++block == r.blocks) {
                 block = 0;
                 if (++head == c.kv_heads) {
@@ -352,7 +363,7 @@ __global__ void __launch_bounds__(kAttThreads, 1) attention_kernel(const __grid_
         const int per_b = c.kv_heads * P.own.blocks;
         int last = 0, mine = 0;   // of the thread's only or last sequence
         for (int b = b0; b < b1; ++b) {
-            last = block_cost(own_tiles(c, c.lens[b]));
+            last = own_cost(c, P.own, c.lens[b]);
             mine += last * per_b;
         }
         int upto = mine;
@@ -376,14 +387,14 @@ __global__ void __launch_bounds__(kAttThreads, 1) attention_kernel(const __grid_
         const bool here = from >= before && from < upto;
         if (tid == 0 && from == to) start = AttStart{0, 0, 0, false, 0, 0, 0};
         if (tid == 0 && from < to && from < P.shared_cost) {
-            const int each = block_cost(P.shared_tiles), item = from / each;
+            const int each = block_cost(head_cost(A.shared_len, P.shared_tiles), P.shared_tiles, P.shared.tile_cost), item = from / each;
             start = AttStart{from, to, item * each, true, 0, item / P.shared.blocks, item % P.shared.blocks};
         }
         if (here && from < to) {
             int b = b0;
             if (per > 1)
                 for (; b < b1; ++b) {
-                    last = block_cost(own_tiles(c, c.lens[b]));
+                    last = own_cost(c, P.own, c.lens[b]);
                     if (from < before + last * per_b) break;
                     before += last * per_b;
                 }
@@ -399,7 +410,7 @@ __global__ void __launch_bounds__(kAttThreads, 1) attention_kernel(const __grid_
             before = upto - mine;
             for (int b = b0; b < b1; ++b) {
                 P.before[b] = before;
-                before += block_cost(own_tiles(c, c.lens[b])) * per_b;
+                before += own_cost(c, P.own, c.lens[b]) * per_b;
             }
             if (b1 == c.batch) P.before[c.batch] = before;
         }
@@ -889,11 +900,12 @@ __global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(const __gr
     const AttTile t = tile_of(K, false, tile);
     const int row0 = chunk * P.join_rows, row1 = min(t.count * static_cast<int>(P.group.d), row0 + P.join_rows);
     if (row0 >= row1) return;
-    const int tiles = own_tiles(c, len), own0 = P.before[b] + (hk * P.own.blocks + block) * block_cost(tiles), all = P.first[P.grid];
+    const int tiles = own_tiles(c, len), own_head = head_cost(min(len, own_end(c, len)), tiles),
+              own0 = P.before[b] + (hk * P.own.blocks + block) * block_cost(own_head, tiles, P.own.tile_cost), all = P.first[P.grid];
     if (!P.shared_tiles) {   // of the CTAs that begin within the block, the first one's task is this
         const int from = P.begin[task].w;
         int i = task - 1, before = 0;
-        while (i > 0 && (before = tiles_before(P.first[i] - own0, tiles)) == from) --i;   // (a run can be too short for a tile)
+        while (i > 0 && (before = tiles_before(P.first[i] - own0, own_head, tiles, P.own.tile_cost)) == from) --i;   // (a run can be too short for a tile)
         if (i > 0 && before > 0) return;
     }
     const int item = (b * c.kv_heads + hk) * P.own.blocks + block;
@@ -910,12 +922,12 @@ __global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(const __gr
         const int in = P.group.quot(row), n = t.node + in, h = hk * P.group.d + (row - in * P.group.d), col = lane * E;
         float ref = neg_inf(), sum = 0.f, o[E] = {};
         // The pieces of a block: of the CTAs from `cta`, whose first rows in the workspace are row_0 + i * by; a lane looks at each.
-        const auto add = [&](int at, int n_tiles, int cta, int64_t row_0, int by, int rows_of, int r) {
+        const auto add = [&](int at, int head, int n_tiles, int tile_cost, int cta, int64_t row_0, int by, int rows_of, int r) {
             const float *src = P.o + row_0 * D + ((col / 32) * rows_of + r) * 32 + ((col % 32 / 4) ^ (r & 7)) * 4 + col % 4;
-            const int end = at + block_cost(n_tiles);
+            const int end = at + block_cost(head, n_tiles, tile_cost);
             for (; cta < P.grid; cta += 32) {
                 const int i = cta + lane, from = i <= P.grid ? P.first[i] : 0x7fffffff, to = i < P.grid ? P.first[i + 1] : 0x7fffffff;
-                const bool piece = i < P.grid && from < end && tiles_before(to - at, n_tiles) > tiles_before(from - at, n_tiles);
+                const bool piece = i < P.grid && from < end && tiles_before(to - at, head, n_tiles, tile_cost) > tiles_before(from - at, head, n_tiles, tile_cost);
                 unsigned left = __ballot_sync(kFull, piece);
                 while (left) {
                     float z[kJoinAtOnce][E];
@@ -956,10 +968,11 @@ __global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(const __gr
             const AttRows &r = P.shared;
             const int node = b * c.nodes + n, period = r.by_period.quot(node), in_p = node - period * r.period, part = r.by_nodes.quot(in_p);
             const int s_tile = period * r.parts + part, s_row = (in_p - part * r.nodes) * P.group.d + (row - in * P.group.d);
-            const int s_item = hk * r.blocks + s_tile / 2, at = s_item * block_cost(P.shared_tiles);
-            add(at, P.shared_tiles, first_cta(at), static_cast<int64_t>(s_item) * s_step + s_tile % 2 * r.slot_rows, s_step, r.slot_rows, s_row);
+            const int s_item = hk * r.blocks + s_tile / 2, s_head = head_cost(A.shared_len, P.shared_tiles);
+            const int at = s_item * block_cost(s_head, P.shared_tiles, r.tile_cost);
+            add(at, s_head, P.shared_tiles, r.tile_cost, first_cta(at), static_cast<int64_t>(s_item) * s_step + s_tile % 2 * r.slot_rows, s_step, r.slot_rows, s_row);
         }
-        add(own0, tiles, own_cta, own_row, step, P.own.slot_rows, row);
+        add(own0, own_head, tiles, P.own.tile_cost, own_cta, own_row, step, P.own.slot_rows, row);
         const bool none = sum == 0.f;
         const float inv = none ? 0.f : 1.f / sum;
         T *dst = static_cast<T *>(A.out.data) + b * A.out.seq + n * A.out.node + h * A.out.head + col;
