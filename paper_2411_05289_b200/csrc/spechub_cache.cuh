@@ -8,7 +8,7 @@
 
 namespace spechub {
 
-constexpr int kAppendThreads = 256;
+constexpr int kAppendThreads = 512;   // at most
 
 // One CTA per node.  An item is 32 bytes of a head: eight pairs (two vectors of eight elements: of both halves of the
 // rotated part, or neighbours), or sixteen elements that are copied.  The node's cosines and sines are found once, for all heads.
@@ -22,20 +22,20 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(const __grid_con
     const int32_t *row = c.table + b * c.stride_table;
     if (n == 0 && c.status) {
         bool bad = false;
-        for (int i = tid; i < c.nodes && len >= 0; i += kAppendThreads) bad |= page_of(c, row, len + i) < 0;
+        for (int i = tid; i < c.nodes && len >= 0; i += blockDim.x) bad |= page_of(c, row, len + i) < 0;
         bad = __syncthreads_or(bad);
         if (tid == 0) c.status[b] = bad ? SPECHUB_ST_PAGE : 0u;
     }
     if (len < 0) return;
     const int half = A.rotated / 2;
-    if (tid < half) {
+    for (int i = tid; i < half; i += blockDim.x) {
         const int64_t d = A.depth ? A.depth[b * A.depth_stride_seq + n] : n;
         // the angle in turns, its whole turns dropped before 32 bits are enough
-        const double turns = static_cast<double>(A.pos_offset + len + d) * (static_cast<double>(A.inv_freq[tid]) * 0.15915494309189535);
+        const double turns = static_cast<double>(A.pos_offset + len + d) * (static_cast<double>(A.inv_freq[i]) * 0.15915494309189535);
         const float f = static_cast<float>(2.0 * (turns - rint(turns)));
         float s, cs;
         sincospif(f, &s, &cs);
-        turn[tid] = make_float2(cs, s);
+        turn[i] = make_float2(cs, s);
     }
     const int page = page_of(c, row, len + n);
     const int64_t place = (len + n) & ((1 << c.page_shift) - 1);
@@ -43,7 +43,7 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(const __grid_con
     __syncthreads();
     const int per_head = c.head_dim / 16, qn = A.q.data ? c.heads * per_head : 0, kn = c.kv_heads * per_head;
     const int rot_items = A.rotated / 16;
-    for (int it = tid; it < qn + 2 * kn; it += kAppendThreads) {
+    for (int it = tid; it < qn + 2 * kn; it += blockDim.x) {
         const int what = it < qn ? 0 : it < qn + kn ? 1 : 2;
         const int j = it - (what == 0 ? 0 : what == 1 ? qn : qn + kn);
         const int h = j / per_head, i = j - h * per_head;
