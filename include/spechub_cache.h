@@ -62,7 +62,7 @@ extern "C" {
 #define SPECHUB_F16 2
 #define SPECHUB_MAX_GROUP 128 /* most query heads per cache head that spechub_tree_attention takes */
 
-#define SPECHUB_ERR_ALIGN (-11)  /* a pointer or stride is not a multiple of 16 bytes, or rows of an output or of the cache overlap */
+#define SPECHUB_ERR_ALIGN (-11)  /* a pointer or stride is not a multiple of 16 bytes, or rows of the cache, of q of spechub_tree_attention or of an output overlap */
 #define SPECHUB_ERR_CACHE (-12)  /* bad cache or head shape: see spechub_cache_desc */
 #define SPECHUB_ERR_ROTARY (-13) /* rotated is not a multiple of 16 from 0 to head_dim, or interleaved is not 0 / 1 */
 #define SPECHUB_ERR_SHARED (-14) /* shared_len < 0, or more tokens than shared_width pages hold */
@@ -130,6 +130,7 @@ int spechub_cache_append(const spechub_cache_desc *desc, const spechub_heads *q,
  * lens[b] + m for which bit m of node n's mask is set.  mask is int32
  * [nodes][ceil(nodes / 32)], bit m % 32 of word m / 32 (mask_stride_seq = 0:
  * one tree for all sequences; otherwise [batch] of them, so many words apart).
+ *   out may not overlap q.  heads / kv_heads is at most SPECHUB_MAX_GROUP.
  *   lse[b][n][h] (may be NULL) is the natural logarithm of sum_j exp(scale * q
  * . k_j).  A row that sees nothing is 0 with lse = -inf.
  *   A key or value that is NaN or infinite concerns the rows that see it only.

@@ -129,6 +129,7 @@ int spechub_tree_attention(const spechub_cache_desc *desc, const spechub_heads *
     if (rc == SPECHUB_OK) rc = heads_of(q, desc, desc->heads, true, &a.q);   // (rows of a tensor copy lie apart)
     if (rc == SPECHUB_OK) rc = heads_of(out, desc, desc->heads, true, &a.out);
     if (rc != SPECHUB_OK) return rc;
+    if (q->data == out->data) return SPECHUB_ERR_ALIGN;   // (queries are read again after the first outputs are there)
     if (!mask || (shared_len > 0 && !shared_table)) return SPECHUB_ERR_NULL;
     size_t need = 0;
     if (!attention_workspace(a.c, shared_len, &need)) return SPECHUB_ERR_SHAPE;

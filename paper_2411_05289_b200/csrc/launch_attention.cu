@@ -100,7 +100,7 @@ bool plan_of(const CacheArgs &c, const HeadsPtr &q, int64_t shared_len, uint8_t 
     p->grid = static_cast<int>(tiles < kSms ? tiles : kSms);
     p->shared_slots = shared_len ? shared_items + p->grid : 0;
     const auto slot = [](const AttRows &r) { return static_cast<int64_t>(r.slot_tiles) * r.slot_rows; };
-    const int64_t own_rows = (own_items + kSms) * slot(p->own);
+    const int64_t own_rows = (shared_len ? own_items + kSms : 2 * kSms) * slot(p->own);   // (without a prefix: a CTA's first and last pieces)
     const int64_t rows = p->shared_slots * slot(p->shared) + own_rows;
     // (the size goes by the shape alone, whichever strides the queries have)
     const auto shared_rows = [&](const AttRows &r) { return shared_len ? (static_cast<int64_t>(c.kv_heads) * r.blocks + kSms) * slot(r) : 0; };

@@ -92,7 +92,7 @@ struct AttPlan {
     AttRows own, shared;          // a sequence's rows; the batch's
     int shared_tiles, grid;       // tiles of keys of the prefix
     int shared_cost;
-    int64_t shared_slots;
+    int64_t shared_slots;         // of the shared blocks' pieces, before those of the own: block + CTA is a piece's number
     bool merged;                  // the batch's nodes are one axis of the queries' shared tensor map, else sequences are its last
     FastDiv group, sequence;      // query heads per cache head; nodes per sequence
     int *before;                  // [batch + 1] cost of the own blocks before sequence b
@@ -590,8 +590,8 @@ __global__ void __launch_bounds__(kAttThreads, 1) attention_kernel(const __grid_
                 const AttRows &r = x.shared ? P.shared : P.own;
                 int64_t row0 = 0;   // in the workspace
                 if (!whole) {
-                    row0 = ((x.item + int64_t(blockIdx.x)) * r.slot_tiles + (x.two ? g : 0)) * r.slot_rows +
-                           (x.shared ? 0 : P.shared_slots * P.shared.slot_tiles * P.shared.slot_rows);
+                    const int64_t slot = P.shared_tiles ? x.item + int64_t(blockIdx.x) : 2 * blockIdx.x + (x.t0 == 0);
+                    row0 = (slot * r.slot_tiles + (x.two ? g : 0)) * r.slot_rows + (x.shared ? 0 : P.shared_slots * P.shared.slot_tiles * P.shared.slot_rows);
                     if (mine && (x.two || g == 0)) P.ml[row0 + gt] = make_float2(ref, sum);
                 } else if (mine && A.lse && (x.two || g == 0)) {
                     A.lse[(static_cast<int64_t>(x.b) * c.nodes + rows.node + in) * c.heads + x.head * P.group.d + (gt - in * P.group.d)] =
@@ -910,7 +910,7 @@ __global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(const __gr
     }
     const int item = (b * c.kv_heads + hk) * P.own.blocks + block;
     const int step = P.own.slot_tiles * P.own.slot_rows, s_step = P.shared.slot_tiles * P.shared.slot_rows;
-    const int64_t own_row = P.shared_slots * s_step + static_cast<int64_t>(item) * step + tb * P.own.slot_rows;
+    const int64_t own_row = P.shared_slots * s_step + (P.shared_tiles ? static_cast<int64_t>(item) * step : 0) + tb * P.own.slot_rows;
     // the first CTA whose run may have tiles of a block whose costs begin at `at`
     const auto first_cta = [&](int at) {
         int i = min(P.grid - 1, at / max(1, all / P.grid));   // (not before the one that has cost `at`, and hardly behind it)
@@ -921,10 +921,12 @@ __global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(const __gr
     for (int row = row0; row < row1; ++row) {
         const int in = P.group.quot(row), n = t.node + in, h = hk * P.group.d + (row - in * P.group.d), col = lane * E;
         float ref = neg_inf(), sum = 0.f, o[E] = {};
-        // The pieces of a block: of the CTAs from `cta`, whose first rows in the workspace are row_0 + i * by; a lane looks at each.
+        // The pieces of a block: of the CTAs from `cta`, a lane looks at each.  Their first rows in the workspace are row_0 + i * by, or where
+        // there is no prefix, and a CTA has two pieces at most, row_0 + (2 i + (whether it is the block's first)) * by.
         const auto add = [&](int at, int head, int n_tiles, int tile_cost, int cta, int64_t row_0, int by, int rows_of, int r) {
             const float *src = P.o + row_0 * D + ((col / 32) * rows_of + r) * 32 + ((col % 32 / 4) ^ (r & 7)) * 4 + col % 4;
             const int end = at + block_cost(head, n_tiles, tile_cost);
+            int begins = P.shared_tiles ? 0 : 1;
             for (; cta < P.grid; cta += 32) {
                 const int i = cta + lane, from = i <= P.grid ? P.first[i] : 0x7fffffff, to = i < P.grid ? P.first[i + 1] : 0x7fffffff;
                 const bool piece = i < P.grid && from < end && tiles_before(to - at, head, n_tiles, tile_cost) > tiles_before(from - at, head, n_tiles, tile_cost);
@@ -938,7 +940,9 @@ __global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(const __gr
 #pragma unroll
                         for (int k = 0; k < E; ++k) z[j][k] = 0.f;
                         if (left) {
-                            const int64_t off = static_cast<int64_t>(cta + __ffs(left) - 1) * by;
+                            const int who = cta + __ffs(left) - 1;
+                            const int64_t off = static_cast<int64_t>(P.shared_tiles ? who : 2 * who + begins) * by;
+                            begins = 0;
                             ml[j] = P.ml[row_0 + off + r];
                             if (E == 4) { const float4 v = *reinterpret_cast<const float4 *>(src + off * D); z[j][0] = v.x; z[j][1] = v.y; z[j][E - 2] = v.z; z[j][E - 1] = v.w; }
                             else { const float2 v = *reinterpret_cast<const float2 *>(src + off * D); z[j][0] = v.x; z[j][1] = v.y; }

@@ -276,6 +276,23 @@ def test_attention(sh, dt, lens, n, hk, g, d, ps, layout, shared):
     c.check(got)
 
 
+@pytest.mark.parametrize("seed", range(6))
+def test_drawn_batches(sh, seed):
+    """Lengths, trees, heads, pages and prefixes as they come."""
+    r = np.random.default_rng(1000 + seed)
+    for _ in range(6):
+        n = int(r.choice([1, 1, 2, 5, 17, 31, 64, 70, 129]))
+        g, hk, d = int(r.choice([1, 2, 3, 4, 5, 8, 16])), int(r.choice([1, 2, 3])), int(r.choice([64, 128]))
+        lens = [int(x) if r.random() > 0.1 else -1 for x in r.integers(0, r.choice([2, 140, 1500]), r.integers(1, 12))]
+        shared = int(r.choice([0, 0, 1, 127, 128, 129, 900]))
+        ps, layout = int(r.choice([8, 16, 32, 64, 128, 256])), str(r.choice(["nhd", "hnd", "pair"]))
+        c = Case(int(r.integers(1 << 30)), lens, n, hk, g, d, ps, str(r.choice(["bf16", "fp16"])), layout, shared,
+                 tree_mask(n, int(r.choice([1, 2, 3]))), strided_q=bool(r.random() < 0.5))
+        got = c.run(sh)
+        assert got["status"].tolist() == [0] * len(lens)
+        c.check(got)
+
+
 @pytest.mark.parametrize("lens,n,hk,g,d,shared", [
     ([40, 7, 300, 0, 12], 7, 2, 4, 128, 300),       # four sequences' rows in a tile
     ([5, 60, 2], 31, 1, 4, 64, 129),                # one
@@ -431,6 +448,21 @@ def test_offsets_beyond_32_bits(sh):
     path = torch.tensor([[0, 2, 4]], dtype=torch.int32, device="cuda")
     assert sh.spechub_cache_accept(cache, cache.clone(), table, lens, path, 5)["lens"].tolist() == [603]
     assert torch.equal(cache[pages - 2, 88:91], k[0, [0, 2, 4]])
+
+
+def test_workspace_stays_small_without_a_prefix(sh):
+    """Two pieces per SM at most, whatever the batch: not one for every block."""
+    import ctypes
+
+    from test_cache_refusals import Desc
+
+    lib = sh.load_library()
+    lib.spechub_tree_attention_workspace_bytes.restype = ctypes.c_size_t
+    size = {}
+    for batch in (64, 4096):
+        d = Desc(ctypes.sizeof(Desc), 1, 1, batch, 31, 32, 8, 128, 16, 10, 1, 100, 100, 4096, 4096)
+        size[batch] = lib.spechub_tree_attention_workspace_bytes(ctypes.byref(d), ctypes.c_int64(0))
+    assert size[4096] < size[64] + 4 * 5000 < 32 << 20
 
 
 def test_results_repeat(sh):

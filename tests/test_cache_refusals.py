@@ -67,7 +67,7 @@ def attend(d=None, q=None, kc=None, vc=None, mask=FAKE, mask_stride=0, shared=No
     lib = sh.load_library()
     return lib.spechub_tree_attention(ref(d or desc()), ref(q or heads()), ref(kc or pages()), ref(vc or pages()), mask,
                                       ctypes.c_int64(mask_stride), shared, width, ctypes.c_int64(shared_len), ctypes.c_float(scale),
-                                      ref(out or heads()), None, None, workspace, ctypes.c_size_t(nbytes), None)
+                                      ref(out or heads(data=16384)), None, None, workspace, ctypes.c_size_t(nbytes), None)
 
 
 def accept(d=None, kc=None, vc=None, path=FAKE, levels=3, lens_out=ctypes.c_void_p(8192)):
@@ -128,6 +128,10 @@ def test_attention_refuses():
     assert attend(mask=None) == -1
     assert attend(mask_stride=2) == -5
     assert attend(desc(layers=2)) == -12
+    assert attend(desc(heads=4 * 129)) == -12                # more query heads per cache head than a tile has rows
+    assert attend(q=heads(head=0)) == -11                    # (queries are copied as a tensor: rows lie apart)
+    same = heads(data=12288)
+    assert attend(q=same, out=same) == -11
     lib = sh.load_library()
     lib.spechub_tree_attention_workspace_bytes.restype = ctypes.c_size_t
     need = lib.spechub_tree_attention_workspace_bytes(ref(desc()), ctypes.c_int64(0))
