@@ -541,10 +541,8 @@ __global__ void __launch_bounds__(kAttThreads, 1) attention_kernel(const __grid_
             // ---- the end of the piece ------------------------------------------------------------------
             AttPiece y = {};
             there = next_piece(y);   // (while the last product runs)
-            if (first < x.t1) {
-                bar_wait(o_full(g), o_phase, gave_up);
-                o_phase ^= 1u;
-            }
+            bar_wait(o_full(g), o_phase, gave_up);
+            o_phase ^= 1u;
             const bool whole = !x.shared && P.shared_tiles == 0 && x.t1 - x.t0 == x.tiles;
             const bool join = !x.two && x.t1 - x.t0 > 1;   // of both groups
             float f0 = 1.f, f1 = 0.f;                      // factors of O: of group 0 (a group's own where it is alone), of group 1
@@ -677,9 +675,7 @@ __global__ void __launch_bounds__(kAttThreads, 1) attention_kernel(const __grid_
                 const int n = x.t1 - x.t0, step = x.two ? 1 : 2, first = x.two ? 0 : g;
                 const uint32_t q = q_n + (x.two ? g : 0);   // the slot of queries
                 q_n += x.two ? 2 : 1;
-                if (x.two && g == 1) bar_wait_one(q_full((q - 1) & 1u), (q - 1) / 2 & 1u, gave_up);
-                bar_wait_one(q_full(q & 1u), q / 2 & 1u, gave_up);
-                if (x.two && g == 0) bar_wait_one(q_full((q + 1) & 1u), (q + 1) / 2 & 1u, gave_up);
+                bar_wait_one(q_full(q & 1u), q / 2 & 1u, gave_up);   // (not the other group's: that may be two rounds on)
                 // Two tiles of rows: the groups' products and scores go in turns, whole.  Mixed, both would be done at the same time, and
                 // both groups would then compute their weights at the same time, and the tensor core would wait for both (5400 clocks
                 // for a tile of keys; in turns 4100).
@@ -688,16 +684,12 @@ __global__ void __launch_bounds__(kAttThreads, 1) attention_kernel(const __grid_
                     bar_wait_one(turn(g), turn_phase, gave_up);
                     turn_phase ^= 1u;
                 };
-                bool o_mine = false;
                 for (int i = first - step; i < n; i += step) {
                     const bool now = i >= first, more = i + step < n;
                     if (now) {
                         pass_v(n0 + i);
                         v_arrived();
-                        if (!o_mine) {   // O of the piece before has been read by now or soon
-                            bar_wait_one(o_free, free_phase, gave_up);
-                            o_mine = true;
-                        }
+                        if (i == first) bar_wait_one(o_free, free_phase, gave_up);   // O of the piece before has been read by now or soon
                     }
                     const uint32_t v_slot = v_n % SV;
                     if (more) pass_k(n0 + i + step);
@@ -736,11 +728,14 @@ __global__ void __launch_bounds__(kAttThreads, 1) attention_kernel(const __grid_
                     }
                     if (now && x.two) mma_commit(v_empty(v_slot));
                 }
-                if (first >= n) bar_arrive(q_empty(q & 1u));
+                if (first >= n) {   // no tile for this group, but its part in the piece: else the others could be two pieces on
+                    bar_arrive(q_empty(q & 1u));
+                    bar_wait_one(o_free, free_phase, gave_up);
+                    bar_arrive(o_full(g));
+                }
                 n0 += n;
                 pass_k(n0);
                 pass_v(n0);
-                if (!o_mine) bar_wait_one(o_free, free_phase, gave_up);
                 free_phase ^= 1u;
             }
             bar_wait_one(o_free, free_phase, gave_up);

@@ -474,6 +474,25 @@ def test_results_repeat(sh):
             assert torch.equal(first[key], again[key])
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("lens,n,g,shared", [
+    ([0] * 13, 31, 32, 5000),        # a block of one tile of rows, then blocks of two with a tile of keys each
+    ([0, 1, 200, 0] * 9, 13, 32, 130),
+    ([0, 300, 1, 0, 129] * 9, 5, 32, 0),
+    ([0, 1] * 100, 1, 8, 0),         # all of one tile
+])
+def test_short_pieces_one_after_the_other(sh, d, lens, n, g, shared):
+    """Pieces of a single tile of keys, which the parts of a block pass at different times."""
+    case = Case(77, lens, n, 1, g, d, 16, shared=shared)
+    first = {k: v.clone() for k, v in case.run(sh).items()}
+    assert not first["status"].any()
+    case.check(first)
+    for _ in range(50):
+        again = case.run(sh)
+        assert not again["status"].any()
+        assert torch.equal(again["out"], first["out"]) and torch.equal(again["lse"], first["lse"])
+
+
 def test_other_streams_and_captured_calls(sh):
     """A captured call is replayed with other lengths, tables and queries; two graphs on two streams do not share anything."""
     c = Case(14, [400, 50, 1], 7, 2, 4, 64, 16, shared=100, mask=tree_mask(7))
