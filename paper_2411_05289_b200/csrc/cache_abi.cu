@@ -24,6 +24,8 @@ int check_cache_desc(const spechub_cache_desc *d) {
     return SPECHUB_OK;
 }
 
+constexpr int64_t kMaxShared = 0x3fffffff;
+
 bool at16(const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
 // A stride as the kernels take it: that of a dimension of size 1 is any.  `apart`: places of the dimension may not be the same.
@@ -102,7 +104,9 @@ int spechub_cache_append(const spechub_cache_desc *desc, const spechub_heads *q,
 }
 
 size_t spechub_tree_attention_workspace_bytes(const spechub_cache_desc *desc, int64_t shared_len) {
-    if (check_cache_desc(desc) != SPECHUB_OK || shared_len < 0 || desc->batch == 0) return 0;
+    if (check_cache_desc(desc) != SPECHUB_OK || desc->heads / desc->kv_heads > SPECHUB_MAX_GROUP || shared_len < 0 || shared_len > kMaxShared ||
+        desc->batch == 0)
+        return 0;
     CacheArgs c = {};
     c.batch = desc->batch; c.nodes = desc->nodes; c.heads = desc->heads; c.kv_heads = desc->kv_heads; c.head_dim = desc->head_dim;
     c.page_shift = __builtin_ctz(static_cast<unsigned>(desc->page_size)); c.table_width = desc->table_width;
@@ -119,7 +123,7 @@ int spechub_tree_attention(const spechub_cache_desc *desc, const spechub_heads *
     if (rc != SPECHUB_OK) return rc;
     if (desc->layers != 1 || desc->heads / desc->kv_heads > SPECHUB_MAX_GROUP) return SPECHUB_ERR_CACHE;
     if (!(scale > 0.f && isfinite(scale))) return SPECHUB_ERR_SCALE;
-    if (shared_len < 0 || shared_len > 0x3fffffffLL || shared_width < 0 || shared_len > static_cast<int64_t>(shared_width) * desc->page_size)
+    if (shared_len < 0 || shared_len > kMaxShared || shared_width < 0 || shared_len > static_cast<int64_t>(shared_width) * desc->page_size)
         return SPECHUB_ERR_SHARED;
     const int64_t words = (desc->nodes + 31) / 32;
     if (mask_stride_seq < 0 || (mask_stride_seq != 0 && mask_stride_seq < words * desc->nodes)) return SPECHUB_ERR_STRIDE;

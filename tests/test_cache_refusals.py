@@ -202,3 +202,11 @@ def test_tensors_off_the_device_are_refused():
         sh.spechub_cache_append(z, z, z, z, z, one, one[0])
     with pytest.raises(TypeError):
         sh.spechub_cache_accept(None, z, one, one[0], one)
+
+
+def test_no_workspace_for_what_is_refused():
+    lib = sh.load_library()
+    lib.spechub_tree_attention_workspace_bytes.restype = ctypes.c_size_t
+    need = lambda d, shared=0: lib.spechub_tree_attention_workspace_bytes(ref(d), ctypes.c_int64(shared))  # noqa: E731
+    assert need(desc(heads=128, kv_heads=1)) > 0 and need(desc(heads=129, kv_heads=1)) == 0 and need(desc(heads=4096, kv_heads=2)) == 0
+    assert need(desc(), -1) == 0 and need(desc(), 1 << 30) == 0 and need(desc(), 1 << 40) == 0
