@@ -66,7 +66,7 @@ extern "C" {
 #define SPECHUB_ERR_CACHE (-12)  /* bad cache or head shape: see spechub_cache_desc */
 #define SPECHUB_ERR_ROTARY (-13) /* rotated is not a multiple of 16 from 0 to head_dim, or interleaved is not 0 / 1 */
 #define SPECHUB_ERR_SHARED (-14) /* shared_len < 0, or more tokens than shared_width pages hold */
-#define SPECHUB_ERR_SCALE (-15)  /* scale is not a finite number > 0 */
+#define SPECHUB_ERR_SCALE (-15)  /* scale is not > 0, or scale * log2(e) is no finite number */
 
 #define SPECHUB_ST_PAGE 128u
 #define SPECHUB_ST_PATH 256u

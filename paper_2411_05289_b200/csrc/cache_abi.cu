@@ -122,7 +122,8 @@ int spechub_tree_attention(const spechub_cache_desc *desc, const spechub_heads *
     int rc = check_cache_desc(desc);
     if (rc != SPECHUB_OK) return rc;
     if (desc->layers != 1 || desc->heads / desc->kv_heads > SPECHUB_MAX_GROUP) return SPECHUB_ERR_CACHE;
-    if (!(scale > 0.f && isfinite(scale))) return SPECHUB_ERR_SCALE;
+    const float scale_log2 = scale * 1.4426950408889634f;
+    if (!(scale > 0.f && isfinite(scale_log2))) return SPECHUB_ERR_SCALE;
     if (shared_len < 0 || shared_len > kMaxShared || shared_width < 0 || shared_len > static_cast<int64_t>(shared_width) * desc->page_size)
         return SPECHUB_ERR_SHARED;
     const int64_t words = (desc->nodes + 31) / 32;
@@ -144,7 +145,7 @@ int spechub_tree_attention(const spechub_cache_desc *desc, const spechub_heads *
     a.mask_stride_seq = mask_stride_seq;
     a.shared_table = shared_table;
     a.shared_len = static_cast<int>(shared_len);
-    a.scale_log2 = scale * 1.4426950408889634f;
+    a.scale_log2 = scale_log2;
     a.lse = lse;
     return launch_attention(desc->dtype, a, workspace, static_cast<cudaStream_t>(stream));
 }

@@ -210,3 +210,8 @@ def test_no_workspace_for_what_is_refused():
     need = lambda d, shared=0: lib.spechub_tree_attention_workspace_bytes(ref(d), ctypes.c_int64(shared))  # noqa: E731
     assert need(desc(heads=128, kv_heads=1)) > 0 and need(desc(heads=129, kv_heads=1)) == 0 and need(desc(heads=4096, kv_heads=2)) == 0
     assert need(desc(), -1) == 0 and need(desc(), 1 << 30) == 0 and need(desc(), 1 << 40) == 0
+
+
+def test_a_scale_whose_exponent_of_two_is_no_number():
+    assert attend(scale=3.0e38) == -15
+    assert attend(scale=2.3e38, nbytes=0) == -7   # (the next check)
