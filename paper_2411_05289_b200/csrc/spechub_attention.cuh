@@ -2,9 +2,9 @@
 //
 // Mathematics.  A block of up to 256 rows (row = (sequence, node, query head of one cache head)) goes over its keys in tiles of
 // 128.  S = Q K^T; per row p = 2^(c s - r), l += sum p, O += P V, with c = scale log2(e) and r the row's reference, at first the
-// maximum of the first tile.  r follows the maximum only when that has outgrown it by kSlack (2^kSlack is far from the end of
-// every type here), and then O and l are scaled by 2^(r_old - r): the division by l at the end makes the result the same.  Pieces of
-// one row are joined by their references: out = sum_j 2^(r_j - R) O_j / sum_j 2^(r_j - R) l_j.
+// maximum of the first kStep keys.  Later maxima are not looked for: r is raised only where the weights of kStep keys sum up to more than
+// kMostSum (far from the end of every type here), to their maximum in whole steps, and O and l are scaled by 2^(r_old - r): the division
+// by l at the end makes the result the same.  Pieces of one row are joined by their references: out = sum_j 2^(r_j - R) O_j / sum_j 2^(r_j - R) l_j.
 //
 // Work.  Rows that share keys are one block: the query heads of a cache head and all nodes of a sequence for its own context (7
 // nodes of 4 heads are 28 rows), and the whole batch for the shared prefix, which is thus read once per 256 rows, from L2 but for the
@@ -42,9 +42,12 @@ constexpr int kPieces = 4, kPieceReaders = 11;   // pieces that are known ahead;
 // Registers of a thread: what the block is launched with, and how its warpgroups share them then (a row of scores is 128).
 constexpr int kLaunchRegs = 168, kSoftmaxRegs = 200, kOtherRegs = 104;
 static_assert(256 * kSoftmaxRegs + 128 * kOtherRegs <= kAttThreads * kLaunchRegs, "the block's own registers");
-constexpr float kSlack = 8.f;
+constexpr float kMostSum = 60000.f;   // of kStep weights, before the reference is raised: each of them is a number in fp16
+// Scores that a thread has in registers at a time (32 / 64 / 128: 64 x 31 nodes behind 8192 shared tokens 370 / 339 / 348 us, 64 sequences of
+// 31 nodes 139 / 139 / 152).
+constexpr int kStep = 64;
 // Weights are stored as 2^bias times themselves.  fp16 has numbers down to 2^-24 only: with the reference 7 below, weights of
-// 2^-31 of the largest still count, and the largest is 2^(7 + kSlack) < 65504.
+// 2^-31 of the largest still count.
 template <class T> struct Weight;
 template <> struct Weight<__nv_bfloat16> { static constexpr bool kBf16 = true; static constexpr float kBias = 0.f; };
 template <> struct Weight<__half> { static constexpr bool kBf16 = false; static constexpr float kBias = 7.f; };
@@ -244,6 +247,50 @@ __device__ __noinline__ void mask_scores(uint32_t t_s, uint4 bits) {
         bits = make_uint4(bits.y, bits.z, bits.w, 0);
     }
     tmem_wait_st();
+}
+
+// A row's new reference, where the weights of kStep scores are too large for the one it has, or it has none yet; and what that multiplies its
+// sum, its `there` weights of the tile (t_p) and its O (t_o) by.  The latter two are done here.  A power of two: weights stay as they were
+// rounded, but for those that become too small for fp16, 2^-31 of the largest.
+constexpr uint32_t kNone = ~0u;
+template <class T, int D>
+__device__ __noinline__ float2 raise_reference(uint32_t t_s, uint32_t t_p, int there, uint32_t t_o, float cs, float ref, bool needed) {
+    float top = neg_inf();
+#pragma unroll 1
+    for (int i = 0; i < kStep; i += 8) {
+        float s[8];
+        tmem_ld8(t_s + i, s);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) top = fmaxf(top, s[j]);
+    }
+    top = top * cs - Weight<T>::kBias;
+    const float up = needed ? fmaxf(0.f, ceilf(top - ref)) : 0.f;   // (a row is what it is whichever rows are in its warp)
+    const float now = ref == neg_inf() ? top : ref + up, f = ref == neg_inf() ? 1.f : up < 126.f ? __int_as_float((127 - static_cast<int>(up)) << 23) : 0.f;
+    if (t_p != kNone) {
+        tmem_wait_st();
+#pragma unroll 1
+        for (int i = 0; i < there; i += 8) {
+            float w[8];
+            tmem_ld8(t_p + i, w);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float2 e = unpack2<T>(__float_as_uint(w[j]));
+                w[j] = __uint_as_float(pack2<T>(e.x * f, e.y * f));
+            }
+            tmem_st8(t_p + i, w);
+        }
+    }
+    if (t_o != kNone)   // (the product that added the last tile to O is done: it was issued before these scores)
+#pragma unroll 1
+        for (int i = 0; i < D; i += 8) {
+            float o[8];
+            tmem_ld8(t_o + i, o);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) o[j] *= f;
+            tmem_st8(t_o + i, o);
+        }
+    tmem_wait_st();
+    return make_float2(now, f);
 }
 
 template <class T> __device__ __forceinline__ bool not_finite(uint16_t e);
@@ -457,6 +504,12 @@ __global__ void __launch_bounds__(kAttThreads, 1) attention_kernel(const __grid_
             tmem_fence_before();
         }
         const float cs = A.scale_log2;
+        float ref = neg_inf(), sum = 0.f;
+        const auto raise = [&](int h, bool first, bool needed) {   // (where `needed` or it has none)
+            const float2 r = raise_reference<T, D>(t_s + kStep * h, h ? t_p : kNone, kStep / 2 * h, first ? kNone : t_o + g * D, cs, ref, needed);
+            ref = r.x;
+            sum *= r.y;
+        };
         uint32_t n0 = 0;   // tiles of values before this piece
         bool there = next_piece(x);
         while (there) {
@@ -464,7 +517,8 @@ __global__ void __launch_bounds__(kAttThreads, 1) attention_kernel(const __grid_
             const AttTile rows = tile_of(K, x.shared, tile);
             const int valid = rows.count * P.group.d, in = P.group.quot(gt);   // rows of the tile; the row's node
             const bool warp_on = gt - lane < valid, mine = gt < valid;           // any row in this warp
-            float ref = neg_inf(), sum = 0.f;
+            ref = neg_inf();
+            sum = 0.f;
             const int step = x.two ? 1 : 2, first = x.two ? x.t0 : x.t0 + g;
             for (int t = first; t < x.t1; t += step) {
                 const bool masked = x.masked(t);
@@ -474,65 +528,40 @@ __global__ void __launch_bounds__(kAttThreads, 1) attention_kernel(const __grid_
                 s_phase ^= 1u;
                 tmem_fence_after();
                 if (warp_on) {
-                    // Loops, and what is rare in functions: in one stretch of code, with all 128 scores in registers, a tile takes 1380
-                    // clocks where it is alone and 1680 as here, but here the warps wait less for their code (502 -> 372 us for 64 x 31
-                    // nodes behind 8192 shared tokens).  Exponentials by a polynomial, for a part of them, bring nothing here.
+                    // A loop, and what is rare in functions: the warps wait less for their code (all 128 scores in one stretch of code and in
+                    // registers: 502 us instead of 372 for 64 x 31 nodes behind 8192 shared tokens).  With a pass of its own for each tile's
+                    // maximum 350 us, without 339.  Exponentials by a polynomial, for a part of them, bring nothing here.
                     if (masked) mask_scores(t_s, bits);
-                    float m0 = neg_inf(), m1 = neg_inf(), m2 = neg_inf(), m3 = neg_inf();
 #pragma unroll 1
-                    for (int h = 0; h < 2; ++h) {
-                        float s[64];
-                        tmem_ld32_async(t_s + 64 * h, s);
-                        tmem_ld32_async(t_s + 64 * h + 32, s + 32);
-                        tmem_wait_ld(s);
-#pragma unroll
-                        for (int i = 0; i < 64; i += 8) {
-                            m0 = max3(m0, s[i], s[i + 1]);
-                            m1 = max3(m1, s[i + 2], s[i + 3]);
-                            m2 = max3(m2, s[i + 4], s[i + 5]);
-                            m3 = max3(m3, s[i + 6], s[i + 7]);
-                        }
-                    }
-                    const float top = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3)) * cs - Weight<T>::kBias;
-                    if (t == first) ref = top;
-                    else if (__any_sync(kFull, top > ref + kSlack && mine)) {
-                        // (the product that added the last tile to O is done: it was issued before these scores)
-                        const float now = fmaxf(ref, top), f = now == neg_inf() ? 1.f : ex2(ref - now);
-                        sum *= f;
-                        ref = now;
+                    for (int h = 0; h < kTile / kStep; ++h) {
+                        if (__any_sync(kFull, mine && ref == neg_inf())) raise(h, t == first, false);
+                        uint32_t w[kStep / 2];
+                        float l;
 #pragma unroll 1
-                        for (int i = 0; i < D; i += 8) {   // (few at a time: the scores are in registers)
-                            float o[8];
-                            tmem_ld8(t_o + g * D + i, o);
+                        for (int tries = 0; tries < 2; ++tries) {
+                            const float sub = !mine ? neg_inf() : ref == neg_inf() ? 0.f : -ref;
+                            const float2 sub2 = make_float2(sub, sub), cs2 = make_float2(cs, cs);
+                            float2 l0 = make_float2(0.f, 0.f), l1 = l0;
+                            float s[kStep];
 #pragma unroll
-                            for (int j = 0; j < 8; ++j) o[j] *= f;
-                            tmem_st8(t_o + g * D + i, o);
-                        }
-                    }
-                    const float sub = !mine ? neg_inf() : ref == neg_inf() ? 0.f : -ref;
-                    const float2 sub2 = make_float2(sub, sub), cs2 = make_float2(cs, cs);
-                    float2 l0 = make_float2(0.f, 0.f), l1 = l0;
-#pragma unroll 1
-                    for (int h = 0; h < 2; ++h) {
-                        float s[64];
-                        tmem_ld32_async(t_s + 64 * h, s);
-                        tmem_ld32_async(t_s + 64 * h + 32, s + 32);
-                        tmem_wait_ld(s);
+                            for (int i = 0; i < kStep; i += 32) tmem_ld32_async(t_s + kStep * h + i, s + i);
+                            tmem_wait_ld(s);
 #pragma unroll
-                        for (int q = 0; q < 2; ++q) {
-                            uint32_t w[16];
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) {
-                                const float2 a = fma2(make_float2(s[32 * q + 2 * i], s[32 * q + 2 * i + 1]), cs2, sub2);
+                            for (int i = 0; i < kStep / 2; ++i) {
+                                const float2 a = fma2(make_float2(s[2 * i], s[2 * i + 1]), cs2, sub2);
                                 const float2 e = make_float2(ex2(a.x), ex2(a.y));
                                 if (i & 1) l1 = add2(l1, e);
                                 else l0 = add2(l0, e);
                                 w[i] = pack2<T>(e.x, e.y);
                             }
-                            tmem_st16_async(t_p + 32 * h + 16 * q, w);   // (over scores that have been read)
+                            l = (l0.x + l0.y) + (l1.x + l1.y);
+                            if (!__any_sync(kFull, l > kMostSum)) break;
+                            raise(h, t == first, l > kMostSum);
                         }
+                        sum += l;
+#pragma unroll
+                        for (int i = 0; i < kStep / 2; i += 16) tmem_st16_async(t_p + kStep / 2 * h + i, w + i);   // (over scores that have been read)
                     }
-                    sum += (l0.x + l0.y) + (l1.x + l1.y);
                     tmem_wait_st();
                     tmem_fence_before();
                 }

@@ -339,6 +339,25 @@ def test_scores_that_grow_along_the_keys(sh):
     c.check(c.run(sh))
 
 
+@pytest.mark.parametrize("dt", ["bf16", "fp16"])
+@pytest.mark.parametrize("d,lens,n,g,shared", [(64, [700, 0, 130], 7, 4, 0), (128, [700, 0, 130], 40, 4, 300), (128, [500], 1, 1, 0), (64, [390], 62, 4, 0)])
+def test_scores_that_jump_within_a_tile(sh, dt, d, lens, n, g, shared):
+    """By 2^10 to 2^100 and back, at places inside tiles and their parts, for some of the rows of a warp only."""
+    c = Case(33, lens, n, 2, g, d, 16, dt, "nhd", shared)
+    u = torch.nn.functional.normalize(torch.randn(d, generator=c.gen, device="cuda"), dim=0)
+    c.q += ((2.0 * d ** 0.5) * u).to(c.dt)
+    c.q[:, ::3] -= ((2.0 * d ** 0.5) * u).to(c.dt)      # (these see no jumps)
+    jumps = ((40, 5.0), (64, 12.0), (70, -9.0), (100, 20.0), (128, 8.0), (190, 30.0), (193, -30.0), (260, 35.0), (383, 33.0), (385, 12.0), (450, 20.0), (640, 30.0))
+    for ids, count in [(c.ids_shared, shared)] + [(c.table[i], x + n) for i, x in enumerate(lens)]:
+        for at, by in jumps:
+            if at < count:
+                page = c.kc[int(ids[at // 16])]
+                page[at % 16] += (by * u).to(c.dt)
+    got = c.run(sh)
+    assert not got["status"].any()
+    c.check(got)
+
+
 def test_masks_of_any_kind(sh):
     """Rows that see no node, only others, or all; one mask per sequence; a context of nothing leaves such rows empty."""
     rng = np.random.default_rng(3)
