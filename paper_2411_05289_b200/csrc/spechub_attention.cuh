@@ -257,11 +257,11 @@ template <class T, int D>
 __device__ __noinline__ float2 raise_reference(uint32_t t_s, uint32_t t_p, int there, uint32_t t_o, float cs, float ref, bool needed) {
     float top = neg_inf();
 #pragma unroll 1
-    for (int i = 0; i < kStep; i += 8) {
-        float s[8];
-        tmem_ld8(t_s + i, s);
+    for (int i = 0; i < kStep; i += 32) {
+        float s[32];
+        tmem_ld32(t_s + i, s);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) top = fmaxf(top, s[j]);
+        for (int j = 0; j < 32; j += 2) top = max3(top, s[j], s[j + 1]);
     }
     top = top * cs - Weight<T>::kBias;
     const float up = needed ? fmaxf(0.f, ceilf(top - ref)) : 0.f;   // (a row is what it is whichever rows are in its warp)
