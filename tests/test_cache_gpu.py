@@ -701,3 +701,11 @@ def test_a_decoding_loop(sh):
         last = out["n_emitted"].long() - 1
         root = emitted.gather(1, last[:, None])[:, 0].long()
     assert moved > 5
+
+
+def test_too_many_query_heads_per_cache_head(sh):
+    c = Case(2, [5, 6], 3, 1, 4, 64, 16)
+    for heads, code in ((129, -12), (4096, -12)):
+        with pytest.raises(sh.SpecHubError) as e:
+            sh.spechub_tree_attention(torch.zeros((2, 3, heads, 64), dtype=c.dt, device="cuda"), c.kc, c.vc, c.pages, c.lens, c.mask)
+        assert e.value.code == code
