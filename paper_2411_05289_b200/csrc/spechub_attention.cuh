@@ -694,6 +694,9 @@ __global__ void __launch_bounds__(kAttThreads, 1) attention_kernel(const __grid_
             __syncwarp();
             if (lane == 0) bar_arrive(o_free);
             if (whole) half_done(x.two ? L::kHalves - 1 : D == 64 ? 0 : g);
+            // Copies to the workspace have read their staging before the warp goes on: the next piece's outputs, those of other warps too, may
+            // take its place (they are written behind barriers of the next piece at which this warp arrives).
+            else if (lane == 0) store_wait_read();
             n0 += x.t1 - x.t0;
             x = y;
         }

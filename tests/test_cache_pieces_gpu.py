@@ -1,0 +1,33 @@
+"""Tree attention: blocks that several CTAs share, and blocks that one CTA finishes, in one CTA's run.  Values and tolerances
+as in test_cache_gpu.py."""
+import pytest
+
+from test_cache_gpu import Case, sh, tree_mask  # noqa: F401  (sh: the fixture)
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+
+@pytest.mark.parametrize("dt", ["bf16", "fp16"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n,g", [(1, 4), (7, 4), (31, 8), (33, 4)])     # a tile of rows, and two
+def test_parts_of_a_block_before_whole_ones(sh, d, n, g, dt):
+    """A CTA hands its part of a long context to the workspace and goes on with short contexts that it finishes itself: both leave through
+    the same shared memory.  Copies beside them keep the memory busy, so that the parts' copies take their time."""
+    lens = ([2500 + 37 * n, 3, 0, 130, 11] + [60, 1] * 3) * 11
+    c = Case(91, lens, n, 2, g, d, 16, dt, mask=tree_mask(n))
+    first = {k: v.clone() for k, v in c.run(sh).items()}
+    assert not first["status"].any()
+    c.check(first)
+    busy, side = torch.empty(1 << 28, dtype=torch.uint8, device="cuda"), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for i in range(30):
+        if i % 5 == 0:
+            with torch.cuda.stream(side):
+                for _ in range(4):
+                    busy[: 1 << 27].copy_(busy[1 << 27:])
+        again = c.run(sh)
+        for key in first:
+            assert torch.equal(again[key], first[key])
+    torch.cuda.synchronize()
