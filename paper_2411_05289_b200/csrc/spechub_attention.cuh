@@ -324,14 +324,13 @@ __device__ __noinline__ void add_not_finite(const AttentionArgs &A, const AttPie
 }
 
 // A tile of values in shared memory, looked through by 128 threads: rows from r1 become zero, and in rows r0..r1 what is no finite number.
-// true: this thread found such.
+// *found is set then, before the place is cleared: the other group may look at the place afterwards, and finds nothing there.
 template <class T, int D>
-__device__ __noinline__ bool clear_values(uint8_t *v, int thread, int r0, int r1) {
+__device__ __noinline__ void clear_values(uint8_t *v, int thread, int r0, int r1, volatile int *found) {
     constexpr int kVecs = D / 8;
     constexpr uint32_t kExp = Weight<T>::kBf16 ? 0x7f807f80u : 0x7c007c00u;   // all ones: no finite number
     const auto place = [&](int i) { return reinterpret_cast<uint4 *>(v + (i % kVecs / 8) * (kTile * 128) + (i / kVecs) * 128 + (i % 8) * 16); };
     for (int i = thread + r1 * kVecs; i < kTile * kVecs; i += kTile) *place(i) = make_uint4(0, 0, 0, 0);
-    bool bad = false;
 #pragma unroll 4
     for (int i = thread + r0 * kVecs; i < r1 * kVecs; i += kTile) {
         uint4 u = *place(i);
@@ -344,10 +343,10 @@ __device__ __noinline__ bool clear_values(uint8_t *v, int thread, int r0, int r1
             if ((w[k] & kExp & 0xffffu) == (kExp & 0xffffu)) w[k] &= 0xffff0000u;
             if ((w[k] & kExp & 0xffff0000u) == (kExp & 0xffff0000u)) w[k] &= 0xffffu;
         }
+        *found = 1;
+        __threadfence_block();
         *place(i) = u;
-        bad = true;
     }
-    return bad;
 }
 
 template <class T, int D>
@@ -576,8 +575,8 @@ __global__ void __launch_bounds__(kAttThreads, 1) attention_kernel(const __grid_
                     // the ring is neither before nor behind this place: these scores came after the last products, these weights are waited for.)
                     const uint32_t n = n0 + t - x.t0;
                     bar_wait(v_full(n % SV), n / SV & 1u, gave_up);
-                    if (clear_values<T, D>(smem + (2 + SK + n % SV) * L::kTileBytes, gt, max(0, x.plain - t * kTile), min(kTile, x.keys - t * kTile)))
-                        *static_cast<volatile int *>(&bad_values) = 1;   // (from here on the CTA looks for such nodes)
+                    // (From here on the CTA looks for such nodes.  Both groups' rows do: who finds a place cleared sees the flag behind this fence.)
+                    clear_values<T, D>(smem + (2 + SK + n % SV) * L::kTileBytes, gt, max(0, x.plain - t * kTile), min(kTile, x.keys - t * kTile), &bad_values);
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     __threadfence_block();
                 }

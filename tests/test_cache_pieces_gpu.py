@@ -31,3 +31,28 @@ def test_parts_of_a_block_before_whole_ones(sh, d, n, g, dt):
         for key in first:
             assert torch.equal(again[key], first[key])
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("dt", ["bf16", "fp16"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n,g,shared", [(31, 8, 0), (40, 4, 130), (70, 3, 0), (7, 4, 0), (1, 8, 40)])
+def test_values_that_are_no_numbers_in_one_and_two_tiles_of_rows(sh, d, n, g, shared, dt):
+    """Every row that sees such a node gets it, whichever of a block's tiles of rows it is in; the other rows keep their bits."""
+    sees = tree_mask(n)
+    c = Case(17, [97, 200, 1, 128 - n // 2], n, 2, g, d, 16, dt, shared=shared, mask=sees)
+    clean = {k: v.clone() for k, v in c.run(sh).items()}
+    c.check(clean)
+    kept = c.vc.clone()
+    for node in sorted({0, n // 3, n - 1}):
+        hit = torch.from_numpy(sees[:, node]).cuda()
+        for bad in (float("nan"), float("inf"), -float("inf")):
+            for i, x in enumerate(c.lens_list):
+                c.vc[int(c.table[i][(x + node) // 16]), (x + node) % 16, 1, d - 3] = bad
+            for _ in range(5):
+                got = c.run(sh)
+                seen = got["out"][:, hit][:, :, g:, d - 3].float()
+                assert bool(seen.isnan().all() if bad != bad else (seen == bad).all())
+                assert torch.equal(got["out"][:, ~hit], clean["out"][:, ~hit]) and torch.equal(got["lse"], clean["lse"])
+                assert torch.equal(got["out"][:, :, :g], clean["out"][:, :, :g])
+                assert torch.equal(got["out"][..., : d - 3], clean["out"][..., : d - 3])
+            c.vc.copy_(kept)
