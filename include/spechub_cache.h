@@ -47,7 +47,13 @@
  * Alignment
  *   Every data pointer to 16-bit elements is a multiple of 16 bytes and every
  *   stride a multiple of 8 elements; the last dimension is contiguous.  A
- *   stride of a dimension of size 1 is not looked at.
+ *   stride of a dimension of size 1 is not looked at.  Strides of the cache, of
+ *   outputs and of q of spechub_tree_attention are at least head_dim.
+ * Overlaps
+ *   Rows (a head of a node, of a token) that a call writes share no element
+ *   with each other; strides for which they do are refused.  (Strides that do
+ *   not nest in each other, which views of a tensor have, are looked at in up to
+ *   4096 steps.)
  */
 #ifndef SPECHUB_CACHE_H_
 #define SPECHUB_CACHE_H_
@@ -62,7 +68,7 @@ extern "C" {
 #define SPECHUB_F16 2
 #define SPECHUB_MAX_GROUP 128 /* most query heads per cache head that spechub_tree_attention takes */
 
-#define SPECHUB_ERR_ALIGN (-11)  /* a pointer or stride is not a multiple of 16 bytes, or rows of the cache, of q of spechub_tree_attention or of an output overlap */
+#define SPECHUB_ERR_ALIGN (-11)  /* a pointer or stride is not a multiple of 16 bytes, or rows overlap: see Overlaps */
 #define SPECHUB_ERR_CACHE (-12)  /* bad cache or head shape: see spechub_cache_desc */
 #define SPECHUB_ERR_ROTARY (-13) /* rotated is not a multiple of 16 from 0 to head_dim, or interleaved is not 0 / 1 */
 #define SPECHUB_ERR_SHARED (-14) /* shared_len < 0, or more tokens than shared_width pages hold */

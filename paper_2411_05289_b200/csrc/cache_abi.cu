@@ -34,6 +34,65 @@ bool stride(int64_t s, int64_t count, int64_t least, bool apart, int64_t *out) {
     return count <= 1 || (s >= (apart ? least : 0) && s % 8 == 0);
 }
 
+// Places of a tensor, or differences of places: sums of index x stride, the index from lo to hi.
+struct Axis {
+    int64_t stride, lo, hi;
+    int64_t low, high;   // the least and the largest sum of the axes behind this one
+};
+
+// Is there a choice of indices, other than all 0 if `other`, whose sum and `at` are less than `width` together, either way?  Axes by falling
+// strides; where they nest, as those of a tensor's views do, each has one index to look at.  Strides that do not nest may take more:
+// after kMostSteps the answer is no.
+constexpr int kMostSteps = 4096;
+bool near(const Axis *x, const Axis *end, int64_t at, int64_t width, bool other, int *steps) {
+    if (x == end) return !other && at < width && at > -width;
+    const auto down = [](int64_t a, int64_t b) { return a / b - (a % b < 0); };   // the quotient's whole part, b > 0
+    const int64_t first = down(-width - (at + x->high), x->stride) + 1, last = -down(at + x->low - width, x->stride) - 1;
+    for (int64_t i = first > x->lo ? first : x->lo; i <= last && i <= x->hi; ++i) {
+        if (--*steps < 0) return false;
+        if (near(x + 1, end, at + x->stride * i, width, other && i == 0, steps)) return true;
+    }
+    return false;
+}
+bool near(Axis *x, int axes, int64_t at, int64_t width, bool other) {
+    int n = 0;
+    for (int i = 0; i < axes; ++i) {   // sorted; axes that lead nowhere are left out
+        const Axis a = x[i];
+        if (a.stride == 0 || (a.lo == 0 && a.hi == 0)) continue;
+        int j = n++;
+        for (; j > 0 && x[j - 1].stride < a.stride; --j) x[j] = x[j - 1];
+        x[j] = a;
+    }
+    constexpr int64_t kMost = 1ll << 58;   // no memory is that large
+    int64_t low = 0, high = 0, by;
+    bool nested = other && at == 0;
+    for (int i = n - 1; i >= 0; --i) {
+        x[i].low = low;
+        x[i].high = high;
+        nested = nested && x[i].stride >= width + high;
+        if (__builtin_mul_overflow(x[i].stride, x[i].lo, &by) || by < -kMost) return false;
+        low += by;
+        if (__builtin_mul_overflow(x[i].stride, x[i].hi, &by) || by > kMost) return false;
+        high += by;
+    }
+    int steps = kMostSteps;
+    return !nested && near(x, x + n, at, width, other, &steps);
+}
+
+// Do two rows of the tensor share an element?
+template <int N>
+bool over_itself(const int64_t (&strides)[N], const int64_t (&counts)[N], int head_dim) {
+    Axis x[N];
+    for (int i = 0; i < N; ++i) x[i] = {strides[i], 1 - counts[i], counts[i] - 1};
+    return near(x, N, 0, head_dim, true);
+}
+bool over_itself(const HeadsPtr &h, const spechub_cache_desc *d, int heads) {
+    return over_itself({h.seq, h.node, h.head}, {d->batch, d->nodes, heads}, d->head_dim);
+}
+bool over_itself(const PagesPtr &p, const spechub_cache_desc *d) {
+    return over_itself({p.layer, p.page, p.token, p.head}, {d->layers, d->pages, d->page_size, d->kv_heads}, d->head_dim);
+}
+
 int heads_of(const spechub_heads *x, const spechub_cache_desc *d, int heads, bool written, HeadsPtr *out) {
     if (!x || !x->data) return SPECHUB_ERR_NULL;
     out->data = x->data;
@@ -95,6 +154,7 @@ int spechub_cache_append(const spechub_cache_desc *desc, const spechub_heads *q,
     }
     if (rc != SPECHUB_OK) return rc;
     if (rotated > 0 && !inv_freq) return SPECHUB_ERR_NULL;
+    if (over_itself(a.c.k, desc) || over_itself(a.c.v, desc) || (q && over_itself(a.q_out, desc, desc->heads))) return SPECHUB_ERR_ALIGN;
     a.depth = depth;
     a.depth_stride_seq = depth_stride_seq;
     a.inv_freq = inv_freq;
@@ -141,6 +201,7 @@ int spechub_tree_attention(const spechub_cache_desc *desc, const spechub_heads *
     if (workspace_bytes < need) return SPECHUB_ERR_WORKSPACE;
     if (need && !workspace) return SPECHUB_ERR_NULL;
     if (need && !at16(workspace)) return SPECHUB_ERR_ALIGN;
+    if (over_itself(a.out, desc, desc->heads)) return SPECHUB_ERR_ALIGN;
     a.mask = mask;
     a.mask_stride_seq = mask_stride_seq;
     a.shared_table = shared_table;
@@ -160,6 +221,7 @@ int spechub_cache_accept(const spechub_cache_desc *desc, const spechub_pages *k_
     rc = cache_args(desc, k_cache, v_cache, status, &a.c);
     if (rc != SPECHUB_OK) return rc;
     if (!path_nodes || !lens_out || lens_out == desc->lens) return SPECHUB_ERR_NULL;
+    if (over_itself(a.c.k, desc) || over_itself(a.c.v, desc)) return SPECHUB_ERR_ALIGN;
     a.path = path_nodes;
     a.levels = levels;
     a.lens_out = lens_out;

@@ -215,3 +215,15 @@ def test_no_workspace_for_what_is_refused():
 def test_a_scale_whose_exponent_of_two_is_no_number():
     assert attend(scale=3.0e38) == -15
     assert attend(scale=2.3e38, nbytes=0) == -7   # (the next check)
+
+
+def test_rows_that_are_written_over_each_other():
+    """Each stride is long enough for a row, and rows meet all the same."""
+    for bad in (dict(node=64), dict(node=7 * 64), dict(seq=64), dict(seq=2 * 8 * 64), dict(head=128), dict(head=96), dict(node=24 * 64 - 8)):
+        assert append(qo=heads(**bad)) == -11, bad
+        assert attend(out=heads(data=1 << 20, **bad)) == -11, bad
+    for bad in (dict(page=64), dict(token=64), dict(token=3 * 64), dict(page=15 * 4 * 64), dict(head=16 * 4 * 64), dict(head=128)):
+        for call in (append, accept):
+            assert call(kc=pages(**bad)) == -11 and call(vc=pages(data=1 << 30, **bad)) == -11, (call.__name__, bad)
+    assert accept(desc(layers=3), kc=pages(layer=64)) == -11
+    assert accept(desc(layers=3), kc=pages(layer=9 * 16 * 4 * 64), vc=pages(layer=10 * 16 * 4 * 64)) == -11

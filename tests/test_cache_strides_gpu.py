@@ -1,0 +1,49 @@
+"""The cache operators' strides: tensors whose strides do not nest, and tensors that lie over themselves."""
+import pytest
+
+from test_cache_gpu import Case, sh, tree_mask  # noqa: F401  (sh: the fixture)
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+
+def test_outputs_whose_strides_do_not_nest(sh):
+    """Rows 0, 2, 4 of one node lie between rows 3, 5, 7 of the next: unusual, but apart."""
+    n, h, d = 2, 3, 64
+    c = Case(1, [100, 40, -1, 300], n, 1, h, d, 16, shared=50, mask=tree_mask(n))
+    want = c.run(sh)
+    c.check(want)
+    room = torch.full((4 * 8 * d,), 3.0, dtype=c.dt, device="cuda")
+    view = room.as_strided((4, n, h, d), (8 * d, 3 * d, 2 * d, 1))
+    c.run(sh, out=dict(out=view, lse=want["lse"].clone(), status=want["status"].clone()))
+    for i in (0, 1, 3):
+        assert torch.equal(view[i], want["out"][i])
+    assert bool((view[2] == 3.0).all())
+    freq = (10000.0 ** (-torch.arange(0, d, 2, dtype=torch.float64) / d)).float().cuda()
+    k = torch.randn((4, n, 1, d), generator=c.gen, device="cuda").to(c.dt)
+    turned = sh.spechub_cache_append(c.q, k, k, c.kc, c.vc, c.pages, c.lens, None, freq)["q"].clone()
+    sh.spechub_cache_append(c.q, k, k, c.kc, c.vc, c.pages, c.lens, None, freq, q_out=view)
+    for i in (0, 1, 3):
+        assert torch.equal(view[i], turned[i])
+
+
+def test_outputs_and_caches_over_themselves_are_refused(sh):
+    n, h, d = 2, 3, 64
+    c = Case(2, [10, 20], n, 1, h, d, 16, mask=tree_mask(n))
+    room = torch.zeros((1 << 16,), dtype=c.dt, device="cuda")
+    lse, status = torch.empty((2, n, h), device="cuda"), torch.empty((2,), dtype=torch.int32, device="cuda")
+    for strides in ((8 * d, d, d, 1), (8 * d, 2 * d, d, 1), (5 * d, 3 * d, d, 1)):
+        view = room.as_strided((2, n, h, d), strides)
+        with pytest.raises(sh.SpecHubError) as e:
+            c.run(sh, out=dict(out=view, lse=lse, status=status))
+        assert e.value.code == -11
+        with pytest.raises(sh.SpecHubError) as e:
+            sh.spechub_cache_append(c.q, c.q[:, :, :1], c.q[:, :, :1], c.kc, c.vc, c.pages, c.lens, q_out=view)
+        assert e.value.code == -11
+    over = room.as_strided((8, 16, 1, d), (8 * d, d, d, 1))
+    path = torch.zeros((2, 1), dtype=torch.int32, device="cuda")
+    with pytest.raises(sh.SpecHubError) as e:
+        sh.spechub_cache_accept(over, room[1 << 15:].as_strided((8, 16, 1, d), (16 * d, d, d, 1)), c.pages, c.lens, path, n)
+    assert e.value.code == -11
+    assert bool((room == 0).all())
