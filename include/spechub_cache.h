@@ -51,9 +51,12 @@
  *   outputs and of q of spechub_tree_attention are at least head_dim.
  * Overlaps
  *   Rows (a head of a node, of a token) that a call writes share no element
- *   with each other; strides for which they do are refused.  (Strides that do
- *   not nest in each other, which views of a tensor have, are looked at in up to
- *   4096 steps.)
+ *   with each other; strides for which they do are refused.  So are a q_out that
+ *   shares elements with k or v, or with q where it is not q itself, and an out
+ *   that does with q.  (Slices of one tensor may lie between each other.  Strides
+ *   that do not nest, as those of views do, are looked at in up to 4096 steps.)
+ *   That outputs, the cache, the workspace and the inputs share nothing else is the
+ *   caller's to see to.
  */
 #ifndef SPECHUB_CACHE_H_
 #define SPECHUB_CACHE_H_
@@ -136,7 +139,7 @@ int spechub_cache_append(const spechub_cache_desc *desc, const spechub_heads *q,
  * lens[b] + m for which bit m of node n's mask is set.  mask is int32
  * [nodes][ceil(nodes / 32)], bit m % 32 of word m / 32 (mask_stride_seq = 0:
  * one tree for all sequences; otherwise [batch] of them, so many words apart).
- *   out may not overlap q.  heads / kv_heads is at most SPECHUB_MAX_GROUP.
+ *   out and q share no element.  heads / kv_heads is at most SPECHUB_MAX_GROUP.
  *   lse[b][n][h] (may be NULL) is the natural logarithm of sum_j exp(scale * q
  * . k_j).  A row that sees nothing is 0 with lse = -inf.
  *   A key or value that is NaN or infinite concerns the rows that see it only.

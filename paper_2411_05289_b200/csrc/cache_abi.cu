@@ -93,6 +93,25 @@ bool over_itself(const PagesPtr &p, const spechub_cache_desc *d) {
     return over_itself({p.layer, p.page, p.token, p.head}, {d->layers, d->pages, d->page_size, d->kv_heads}, d->head_dim);
 }
 
+// Does a row of one tensor share an element with a row of another?
+template <int N>
+bool meet(const void *a, const int64_t (&a_strides)[N], const int64_t (&a_counts)[N], const void *b, const int64_t (&b_strides)[N],
+          const int64_t (&b_counts)[N], int head_dim) {
+    Axis x[2 * N];
+    int n = 0;
+    for (int i = 0; i < N; ++i) {
+        if (a_strides[i] == b_strides[i]) x[n++] = {a_strides[i], 1 - b_counts[i], a_counts[i] - 1};
+        else {
+            x[n++] = {a_strides[i], 0, a_counts[i] - 1};
+            x[n++] = {b_strides[i], 1 - b_counts[i], 0};
+        }
+    }
+    return near(x, n, (static_cast<const char *>(a) - static_cast<const char *>(b)) / 2, head_dim, false);
+}
+bool meet(const HeadsPtr &a, int a_heads, const HeadsPtr &b, int b_heads, const spechub_cache_desc *d) {
+    return meet(a.data, {a.seq, a.node, a.head}, {d->batch, d->nodes, a_heads}, b.data, {b.seq, b.node, b.head}, {d->batch, d->nodes, b_heads}, d->head_dim);
+}
+
 int heads_of(const spechub_heads *x, const spechub_cache_desc *d, int heads, bool written, HeadsPtr *out) {
     if (!x || !x->data) return SPECHUB_ERR_NULL;
     out->data = x->data;
@@ -155,6 +174,12 @@ int spechub_cache_append(const spechub_cache_desc *desc, const spechub_heads *q,
     if (rc != SPECHUB_OK) return rc;
     if (rotated > 0 && !inv_freq) return SPECHUB_ERR_NULL;
     if (over_itself(a.c.k, desc) || over_itself(a.c.v, desc) || (q && over_itself(a.q_out, desc, desc->heads))) return SPECHUB_ERR_ALIGN;
+    if (q) {
+        const bool in_place = a.q_out.data == a.q.data && a.q_out.seq == a.q.seq && a.q_out.node == a.q.node && a.q_out.head == a.q.head;
+        if ((!in_place && meet(a.q_out, desc->heads, a.q, desc->heads, desc)) || meet(a.q_out, desc->heads, a.k, desc->kv_heads, desc) ||
+            meet(a.q_out, desc->heads, a.v, desc->kv_heads, desc))
+            return SPECHUB_ERR_ALIGN;
+    }
     a.depth = depth;
     a.depth_stride_seq = depth_stride_seq;
     a.inv_freq = inv_freq;
@@ -194,14 +219,14 @@ int spechub_tree_attention(const spechub_cache_desc *desc, const spechub_heads *
     if (rc == SPECHUB_OK) rc = heads_of(q, desc, desc->heads, true, &a.q);   // (rows of a tensor copy lie apart)
     if (rc == SPECHUB_OK) rc = heads_of(out, desc, desc->heads, true, &a.out);
     if (rc != SPECHUB_OK) return rc;
-    if (q->data == out->data) return SPECHUB_ERR_ALIGN;   // (queries are read again after the first outputs are there)
     if (!mask || (shared_len > 0 && !shared_table)) return SPECHUB_ERR_NULL;
     size_t need = 0;
     if (!attention_workspace(a.c, shared_len, &need)) return SPECHUB_ERR_SHAPE;
     if (workspace_bytes < need) return SPECHUB_ERR_WORKSPACE;
     if (need && !workspace) return SPECHUB_ERR_NULL;
     if (need && !at16(workspace)) return SPECHUB_ERR_ALIGN;
-    if (over_itself(a.out, desc, desc->heads)) return SPECHUB_ERR_ALIGN;
+    // (queries are read again after the first outputs are there)
+    if (over_itself(a.out, desc, desc->heads) || meet(a.out, desc->heads, a.q, desc->heads, desc)) return SPECHUB_ERR_ALIGN;
     a.mask = mask;
     a.mask_stride_seq = mask_stride_seq;
     a.shared_table = shared_table;

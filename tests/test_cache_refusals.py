@@ -227,3 +227,18 @@ def test_rows_that_are_written_over_each_other():
             assert call(kc=pages(**bad)) == -11 and call(vc=pages(data=1 << 30, **bad)) == -11, (call.__name__, bad)
     assert accept(desc(layers=3), kc=pages(layer=64)) == -11
     assert accept(desc(layers=3), kc=pages(layer=9 * 16 * 4 * 64), vc=pages(layer=10 * 16 * 4 * 64)) == -11
+
+
+def test_outputs_over_inputs():
+    """Rows of 128 bytes, nodes of 8 rows, sequences of 3 nodes."""
+    for far in (128, 1024, 16, 5 * 1024 + 7 * 128 + 112, -16):
+        assert attend(q=heads(data=1 << 20), out=heads(data=(1 << 20) + far)) == -11, far
+        assert append(q=heads(data=1 << 20), qo=heads(data=(1 << 20) + far)) == -11, far
+    assert attend(q=heads(data=1 << 20), out=heads(data=1 << 20, head=72, node=8 * 72, seq=3 * 8 * 72)) == -11   # other strides
+    assert append(q=heads(data=1 << 20), qo=heads(data=1 << 20, head=72, node=8 * 72, seq=3 * 8 * 72)) == -11
+    packed = dict(node=16 * 64, seq=3 * 16 * 64)      # 8 heads of q, 4 of k, 4 of v
+    at = lambda head: heads(data=(1 << 20) + 128 * head, **packed)  # noqa: E731
+    assert append(q=at(0), k=at(8), v=at(12), qo=at(1)) == -11      # over q, not q itself
+    assert append(q=at(0), k=at(8), v=at(12), qo=at(4)) == -11
+    assert append(q=heads(data=1 << 24), k=at(8), v=heads(data=1 << 22), qo=at(1)) == -11      # the last head lies on k's first
+    assert append(q=heads(data=1 << 24), k=heads(data=1 << 22), v=at(12), qo=at(6)) == -11

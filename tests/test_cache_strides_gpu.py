@@ -47,3 +47,30 @@ def test_outputs_and_caches_over_themselves_are_refused(sh):
         sh.spechub_cache_accept(over, room[1 << 15:].as_strided((8, 16, 1, d), (16 * d, d, d, 1)), c.pages, c.lens, path, n)
     assert e.value.code == -11
     assert bool((room == 0).all())
+
+
+def test_slices_of_one_tensor_side_by_side(sh):
+    """Queries, outputs, keys and values that lie between each other in one tensor share nothing, and are taken."""
+    b, n, hk, g, d = 3, 5, 2, 2, 64
+    c = Case(3, [30, 0, 200], n, hk, g, d, 16, mask=tree_mask(n))
+    want = c.run(sh)
+    c.check(want)
+    h = hk * g
+    room = torch.full((b, n, 2 * h + 2 * hk, d), 3.0, dtype=c.dt, device="cuda")
+    q, out, k, v = room[:, :, :h], room[:, :, h:2 * h], room[:, :, 2 * h:2 * h + hk], room[:, :, 2 * h + hk:]
+    q.copy_(c.q)
+    got = sh.spechub_tree_attention(q, c.kc, c.vc, c.pages, c.lens, c.mask, out=dict(out=out, lse=want["lse"].clone(), status=want["status"].clone()))
+    assert torch.equal(got["out"], want["out"]) and torch.equal(q, c.q) and bool((k == 3.0).all())
+    freq = (10000.0 ** (-torch.arange(0, d, 2, dtype=torch.float64) / d)).float().cuda()
+    turned = sh.spechub_cache_append(c.q, k.clone(), v.clone(), c.kc, c.vc, c.pages, c.lens, None, freq)["q"]
+    sh.spechub_cache_append(q, k, v, c.kc, c.vc, c.pages, c.lens, None, freq, q_out=out)
+    assert torch.equal(out, turned) and torch.equal(q, c.q)
+    sh.spechub_cache_append(q, k, v, c.kc, c.vc, c.pages, c.lens, None, freq, q_out=q)
+    assert torch.equal(q, turned)
+    for bad in (room[:, :, 1:h + 1], room[:, :, h + 1:2 * h + 1]):
+        with pytest.raises(sh.SpecHubError) as e:
+            sh.spechub_cache_append(q, k, v, c.kc, c.vc, c.pages, c.lens, None, freq, q_out=bad)
+        assert e.value.code == -11
+    with pytest.raises(sh.SpecHubError) as e:
+        sh.spechub_tree_attention(q, c.kc, c.vc, c.pages, c.lens, c.mask, out=dict(out=room[:, :, 1:h + 1], lse=want["lse"], status=want["status"]))
+    assert e.value.code == -11
