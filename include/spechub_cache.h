@@ -53,7 +53,8 @@
  *   Rows (a head of a node, of a token) that a call writes share no element
  *   with each other; strides for which they do are refused.  So are a q_out that
  *   shares elements with k or v, or with q where it is not q itself, and an out
- *   that does with q.  (Slices of one tensor may lie between each other.  Strides
+ *   that does with q; and, by spechub_cache_accept, keys that share elements with
+ *   values.  (Slices of one tensor may lie between each other.  Strides
  *   that do not nest, as those of views do, are looked at in up to 4096 steps.)
  *   That outputs, the cache, the workspace and the inputs share nothing else is the
  *   caller's to see to.

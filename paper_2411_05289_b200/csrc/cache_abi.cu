@@ -111,6 +111,10 @@ bool meet(const void *a, const int64_t (&a_strides)[N], const int64_t (&a_counts
 bool meet(const HeadsPtr &a, int a_heads, const HeadsPtr &b, int b_heads, const spechub_cache_desc *d) {
     return meet(a.data, {a.seq, a.node, a.head}, {d->batch, d->nodes, a_heads}, b.data, {b.seq, b.node, b.head}, {d->batch, d->nodes, b_heads}, d->head_dim);
 }
+bool meet(const PagesPtr &a, const PagesPtr &b, const spechub_cache_desc *d) {
+    return meet(a.data, {a.layer, a.page, a.token, a.head}, {d->layers, d->pages, d->page_size, d->kv_heads}, b.data, {b.layer, b.page, b.token, b.head},
+                {d->layers, d->pages, d->page_size, d->kv_heads}, d->head_dim);
+}
 
 int heads_of(const spechub_heads *x, const spechub_cache_desc *d, int heads, bool written, HeadsPtr *out) {
     if (!x || !x->data) return SPECHUB_ERR_NULL;
@@ -246,7 +250,8 @@ int spechub_cache_accept(const spechub_cache_desc *desc, const spechub_pages *k_
     rc = cache_args(desc, k_cache, v_cache, status, &a.c);
     if (rc != SPECHUB_OK) return rc;
     if (!path_nodes || !lens_out || lens_out == desc->lens) return SPECHUB_ERR_NULL;
-    if (over_itself(a.c.k, desc) || over_itself(a.c.v, desc)) return SPECHUB_ERR_ALIGN;
+    // (entries of keys that are values too would be moved twice, the second time perhaps after what they were is gone)
+    if (over_itself(a.c.k, desc) || over_itself(a.c.v, desc) || meet(a.c.k, a.c.v, desc)) return SPECHUB_ERR_ALIGN;
     a.path = path_nodes;
     a.levels = levels;
     a.lens_out = lens_out;

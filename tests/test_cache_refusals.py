@@ -242,3 +242,15 @@ def test_outputs_over_inputs():
     assert append(q=at(0), k=at(8), v=at(12), qo=at(4)) == -11
     assert append(q=heads(data=1 << 24), k=at(8), v=heads(data=1 << 22), qo=at(1)) == -11      # the last head lies on k's first
     assert append(q=heads(data=1 << 24), k=heads(data=1 << 22), v=at(12), qo=at(6)) == -11
+
+
+def test_accept_refuses_keys_that_are_values():
+    """Two threads would move the same entries, one perhaps after the other has replaced what it reads."""
+    far = 10 * 16 * 4 * 128                             # bytes of the keys
+    assert accept(vc=pages()) == -11                    # the keys themselves
+    assert accept(vc=pages(data=4096 + far - 128)) == -11
+    assert accept(vc=pages(data=4096 + far - 16)) == -11
+    assert accept(kc=pages(head=16 * 64, token=64)) == -11                                    # the other order of a page, of the same bytes
+    side = dict(page=16 * 4 * 128, token=4 * 128, head=128)
+    assert accept(kc=pages(**side), vc=pages(data=4096 + 112, **side)) == -11                 # side by side, but for 16 bytes
+    assert accept(desc(layers=2), kc=pages(layer=1 << 20), vc=pages(data=4096 + (1 << 21), layer=1 << 20)) == -11   # the values are the second layer

@@ -74,3 +74,24 @@ def test_slices_of_one_tensor_side_by_side(sh):
     with pytest.raises(sh.SpecHubError) as e:
         sh.spechub_tree_attention(q, c.kc, c.vc, c.pages, c.lens, c.mask, out=dict(out=room[:, :, 1:h + 1], lse=want["lse"], status=want["status"]))
     assert e.value.code == -11
+
+
+def test_accept_of_keys_and_values_in_one_tensor(sh):
+    """Heads of keys and of values in turn, and one behind the other; the same tensor twice is refused."""
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    table, lens = torch.tensor([[2, 0], [1, 3]], dtype=torch.int32, device="cuda"), torch.tensor([3, 12], dtype=torch.int32, device="cuda")
+    path = torch.tensor([[0, 2, 5], [0, 1, 3]], dtype=torch.int32, device="cuda")
+    kv = torch.randn((3, 4, 16, 4, 64), generator=gen, device="cuda").bfloat16()
+    want = kv.clone()
+    for i in range(2):
+        for to, node in enumerate(path[i].tolist()):
+            src, dst = int(lens[i]) + node, int(lens[i]) + to
+            want[:, int(table[i, dst // 16]), dst % 16] = kv[:, int(table[i, src // 16]), src % 16]
+    for k, v in ((slice(0, None, 2), slice(1, None, 2)), (slice(0, 2), slice(2, 4))):
+        got = kv.clone()
+        r = sh.spechub_cache_accept(got[..., k, :], got[..., v, :], table, lens, path, 7)
+        assert r["lens"].tolist() == [6, 15] and r["status"].tolist() == [0, 0]
+        assert torch.equal(got, want)
+    with pytest.raises(sh.SpecHubError) as e:
+        sh.spechub_cache_accept(kv, kv, table, lens, path, 7)
+    assert e.value.code == -11
