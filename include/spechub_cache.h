@@ -164,7 +164,8 @@ int spechub_tree_attention(const spechub_cache_desc *desc, const spechub_heads *
  * walk leaves (spechub_seq_out): the visited nodes, then -1.  In every layer
  * the entry of slot lens[b] + path_nodes[b][d] moves to slot lens[b] + d;
  * lens_out[b] = lens[b] + the number of visited nodes (lens[b] itself for an
- * absent sequence).  lens_out must not be lens.  The entries need no other
+ * absent sequence).  lens_out may not overlap lens (SPECHUB_ERR_NULL, as if it
+ * were not given).  The entries need no other
  * rotation: a node's position goes by its depth, which is its place in the
  * path.  (The slots behind the path keep what they hold.)
  */

@@ -249,7 +249,8 @@ int spechub_cache_accept(const spechub_cache_desc *desc, const spechub_pages *k_
     AcceptArgs a = {};
     rc = cache_args(desc, k_cache, v_cache, status, &a.c);
     if (rc != SPECHUB_OK) return rc;
-    if (!path_nodes || !lens_out || lens_out == desc->lens) return SPECHUB_ERR_NULL;
+    // (one CTA writes the new length while others still read the old ones)
+    if (!path_nodes || !lens_out || (lens_out < desc->lens + desc->batch && desc->lens < lens_out + desc->batch)) return SPECHUB_ERR_NULL;
     // (entries of keys that are values too would be moved twice, the second time perhaps after what they were is gone)
     if (over_itself(a.c.k, desc) || over_itself(a.c.v, desc) || meet(a.c.k, a.c.v, desc)) return SPECHUB_ERR_ALIGN;
     a.path = path_nodes;

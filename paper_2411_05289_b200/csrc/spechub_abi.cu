@@ -630,7 +630,7 @@ size_t spechub_draft_stats_bytes(const spechub_desc *desc) {
 const char *spechub_status_string(int code) {
     switch (code) {
         case SPECHUB_OK: return "ok";
-        case SPECHUB_ERR_NULL: return "a required pointer is NULL";
+        case SPECHUB_ERR_NULL: return "a required pointer is NULL (spechub_cache_accept: or lens_out overlaps lens)";
         case SPECHUB_ERR_VERSION: return "descriptor struct_size/version mismatch";
         case SPECHUB_ERR_SHAPE: return "bad shape: need batch >= 0, nodes >= 1, vocab >= 2, 2 <= k <= 8 (k == 2 for SpecHub), levels >= 1, valid flags";
         case SPECHUB_ERR_DTYPE: return "dtype must be SPECHUB_F32 or SPECHUB_BF16 (the cache operators: SPECHUB_BF16 or SPECHUB_F16)";

@@ -254,3 +254,11 @@ def test_accept_refuses_keys_that_are_values():
     side = dict(page=16 * 4 * 128, token=4 * 128, head=128)
     assert accept(kc=pages(**side), vc=pages(data=4096 + 112, **side)) == -11                 # side by side, but for 16 bytes
     assert accept(desc(layers=2), kc=pages(layer=1 << 20), vc=pages(data=4096 + (1 << 21), layer=1 << 20)) == -11   # the values are the second layer
+
+
+def test_accept_refuses_new_lengths_over_the_old_ones():
+    for at in (4096, 4100, 4092):                       # two lengths of 4 bytes
+        assert accept(lens_out=ctypes.c_void_p(at)) == -1, at
+    assert "lens_out" in sh.status_string(-1)
+    assert accept(lens_out=ctypes.c_void_p(4104), kc=pages(token=64)) == -11      # (the next check)
+    assert accept(lens_out=ctypes.c_void_p(4088), kc=pages(token=64)) == -11
