@@ -77,6 +77,7 @@ extern "C" {
 #define SPECHUB_ERR_ROTARY (-13) /* rotated is not a multiple of 16 from 0 to head_dim, or interleaved is not 0 / 1 */
 #define SPECHUB_ERR_SHARED (-14) /* shared_len < 0, or more tokens than shared_width pages hold */
 #define SPECHUB_ERR_SCALE (-15)  /* scale is not > 0, or scale * log2(e) is no finite number */
+#define SPECHUB_ERR_WORK (-16)   /* more work than one call of spechub_tree_attention counts: see there */
 
 #define SPECHUB_ST_PAGE 128u
 #define SPECHUB_ST_PATH 256u
@@ -151,6 +152,13 @@ int spechub_cache_append(const spechub_cache_desc *desc, const spechub_heads *q,
  *   workspace: device scratch, 16-byte aligned, of at least
  * spechub_tree_attention_workspace_bytes(desc, shared_len) bytes.  It need not
  * be cleared; calls that may overlap need one each.
+ *   The work is counted on the host, before the lengths are known: 8 and at most 14
+ * for every 128 keys, for each cache head and each block of up to 256 rows (nodes
+ * times heads / kv_heads; of a sequence with the keys that its whole row of the
+ * table holds, of the batch with the prefix).  Above 2e9, some seconds if the
+ * tables are full, the call is refused (SPECHUB_ERR_WORK).
+ * spechub_tree_attention_workspace_bytes is 0 then, as for an empty batch and for
+ * what else it knows to be refused; otherwise it is not.
  */
 size_t spechub_tree_attention_workspace_bytes(const spechub_cache_desc *desc, int64_t shared_len);
 int spechub_tree_attention(const spechub_cache_desc *desc, const spechub_heads *q, const spechub_pages *k_cache,

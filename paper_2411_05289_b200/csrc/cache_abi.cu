@@ -225,7 +225,7 @@ int spechub_tree_attention(const spechub_cache_desc *desc, const spechub_heads *
     if (rc != SPECHUB_OK) return rc;
     if (!mask || (shared_len > 0 && !shared_table)) return SPECHUB_ERR_NULL;
     size_t need = 0;
-    if (!attention_workspace(a.c, shared_len, &need)) return SPECHUB_ERR_SHAPE;
+    if (!attention_workspace(a.c, shared_len, &need)) return SPECHUB_ERR_WORK;
     if (workspace_bytes < need) return SPECHUB_ERR_WORKSPACE;
     if (need && !workspace) return SPECHUB_ERR_NULL;
     if (need && !at16(workspace)) return SPECHUB_ERR_ALIGN;

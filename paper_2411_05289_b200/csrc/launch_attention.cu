@@ -1,4 +1,5 @@
 // Attention of tree nodes over a paged cache: tensor maps, workspace, launches.
+#include <algorithm>
 #include <mutex>
 
 #include "spechub_attention.cuh"
@@ -68,9 +69,12 @@ AttRows rows_of(int head_dim, int64_t group, int64_t nodes, int64_t period, int6
     return r;
 }
 
+constexpr double kMostCost = 2.0e9;   // of a call
+
 size_t up(size_t n) { return (n + 255) & ~size_t(255); }
 
-// The plan, and the workspace's size; its parts are at `base`.  false: costs are counted in 31 bits, and there may be more than that.
+// The plan, and the workspace's size; its parts are at `base`.  false: costs are counted in 31 bits, and there may be more than that (by the
+// shape alone, as the size: with either layout of the prefix's rows, every context as long as its table, every tile of keys masked).
 bool plan_of(const CacheArgs &c, const HeadsPtr &q, int64_t shared_len, uint8_t *base, AttPlan *p, size_t *bytes) {
     const int64_t group = c.heads / c.kv_heads, most_nodes = kTile / group, all = static_cast<int64_t>(c.batch) * c.nodes;
     const int64_t own_nodes = c.nodes < most_nodes ? c.nodes : most_nodes;
@@ -87,10 +91,10 @@ bool plan_of(const CacheArgs &c, const HeadsPtr &q, int64_t shared_len, uint8_t 
     const int64_t own_items = static_cast<int64_t>(c.batch) * c.kv_heads * p->own.blocks;
     const int64_t shared_items = shared_len ? static_cast<int64_t>(c.kv_heads) * p->shared.blocks : 0;
     const int64_t own_tiles = ((static_cast<int64_t>(c.table_width) << c.page_shift) + kTile - 1) / kTile;   // of a sequence, at most
-    // (at most every tile of keys is masked)
     const auto cost = [](const AttRows &r, double tiles) { return kBlockCost + tiles * (r.tile_cost + kMaskedCost); };
-    const double most = double(shared_items) * cost(p->shared, p->shared_tiles) + double(own_items) * cost(p->own, double(own_tiles));
-    if (most > 2.0e9) return false;
+    const auto shared_most = [&](const AttRows &r) { return shared_len ? double(c.kv_heads) * r.blocks * cost(r, p->shared_tiles) : 0.; };
+    const double own_most = double(own_items) * cost(p->own, double(own_tiles));
+    if (std::max(shared_most(merged), shared_most(apart)) + own_most > kMostCost) return false;
     const int64_t masked = p->shared_tiles - shared_len / kTile;
     p->shared_cost = static_cast<int>(shared_items * (kBlockCost + masked * kMaskedCost + static_cast<int64_t>(p->shared.tile_cost) * p->shared_tiles));
     p->group = FastDiv::of(static_cast<uint32_t>(group));
@@ -160,7 +164,7 @@ int launch_attention(int dtype, const AttentionArgs &a, void *workspace, cudaStr
     AttKernelArgs k;
     k.a = a;
     size_t bytes;
-    if (!plan_of(a.c, a.q, a.shared_len, static_cast<uint8_t *>(workspace), &k.p, &bytes)) return SPECHUB_ERR_SHAPE;
+    if (!plan_of(a.c, a.q, a.shared_len, static_cast<uint8_t *>(workspace), &k.p, &bytes)) return SPECHUB_ERR_WORK;
     const CacheArgs &c = a.c;
     const AttRows &sh = k.p.shared;
     AttMaps maps;

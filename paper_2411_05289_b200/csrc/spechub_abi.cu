@@ -644,6 +644,7 @@ const char *spechub_status_string(int code) {
         case SPECHUB_ERR_ROTARY: return "rotated must be a multiple of 16 from 0 to head_dim, interleaved 0 or 1";
         case SPECHUB_ERR_SHARED: return "shared_len must be >= 0 and fit into the shared pages";
         case SPECHUB_ERR_SCALE: return "scale must be finite and > 0";
+        case SPECHUB_ERR_WORK: return "more work than one call of spechub_tree_attention counts, with every context as long as its row of the table: a narrower table, or fewer sequences or nodes per call";
         case SPECHUB_ERR_TOO_LARGE: return "batch * nodes exceeds SPECHUB_STATIC_MAX_ROWS of spechub_verify_tree_static";
         default: return "unknown status";
     }

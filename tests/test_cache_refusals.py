@@ -262,3 +262,20 @@ def test_accept_refuses_new_lengths_over_the_old_ones():
     assert "lens_out" in sh.status_string(-1)
     assert accept(lens_out=ctypes.c_void_p(4104), kc=pages(token=64)) == -11      # (the next check)
     assert accept(lens_out=ctypes.c_void_p(4088), kc=pages(token=64)) == -11
+
+
+def test_more_work_than_a_call_counts():
+    """By the table's width and the prefix alone, the same for the workspace's size and for the call, whatever the strides."""
+    lib = sh.load_library()
+    lib.spechub_tree_attention_workspace_bytes.restype = ctypes.c_size_t
+    need = lambda d, shared=0: lib.spechub_tree_attention_workspace_bytes(ref(d), ctypes.c_int64(shared))  # noqa: E731
+    rows = lambda d, gap, at: heads(data=at, seq=d.nodes * d.heads * 64 + gap, node=d.heads * 64)  # noqa: E731
+    wide = dict(batch=128, nodes=8192, heads=64, kv_heads=8, table_width=8192, stride_table=8192)
+    for shared, taken, d in ((0, False, desc(**wide)), (0, True, desc(**{**wide, "table_width": 80})),
+                             (6400000, False, desc(batch=1024, nodes=65, heads=8, kv_heads=8)),      # 65 rows in a tile, or 128
+                             (3200000, True, desc(batch=1024, nodes=65, heads=8, kv_heads=8))):
+        assert (need(d, shared) > 0) == taken
+        for gap in (0, 64):
+            args = dict(q=rows(d, gap, 1 << 30), out=rows(d, gap, 1 << 45), shared=FAKE, width=400000, shared_len=shared)
+            assert attend(d, nbytes=0, **args) == (-7 if taken else -16), (taken, gap)
+    assert "table" in sh.status_string(-16)
