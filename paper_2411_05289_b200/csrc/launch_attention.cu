@@ -147,9 +147,9 @@ int launch_type(const AttKernelArgs &k, const AttMaps &maps, cudaStream_t s) {
     if (lrc != SPECHUB_OK) return lrc;
     const AttRows &r = k.p.own;
     const int64_t blocks = k.p.shared_tiles ? static_cast<int64_t>(k.a.c.batch) * k.a.c.kv_heads * r.blocks : k.p.grid;
+    // (no more than there are rows, of which the host takes 31 bits)
     const int64_t tasks = blocks * r.slot_tiles * ((r.slot_rows + k.p.join_rows - 1) / k.p.join_rows), per = kJoinThreads / 32;
     const int64_t grid = (tasks + per - 1) / per + (k.a.c.status ? k.a.c.batch : 0);
-    if (tasks > 0x7fffffffLL) return SPECHUB_ERR_SHAPE;
     return launch_grid(attention_join_kernel<T, D>, static_cast<unsigned>(grid), kJoinThreads, 0, 1, s, k);
 }
 
