@@ -3,7 +3,9 @@ from __future__ import annotations
 
 import glob
 import os
+import re
 import subprocess
+import sys
 from concurrent.futures import ThreadPoolExecutor
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -40,6 +42,23 @@ def is_stale() -> bool:
     return _older(LIB_PATH, sources() + _headers())
 
 
+def registers_of(log: str) -> dict:
+    """Registers a thread of every kernel (mangled name) that ``-Xptxas -v`` tells of."""
+    return {name: int(used) for name, used in re.findall(r"Compiling entry function '([^']+)' for(?:(?!Compiling entry).)*?Used (\d+) registers", log, re.S)}
+
+
+def check_registers(src: str, log: str) -> None:
+    """The attention kernel's warps share out the registers that its blocks are launched with: with another number it must not
+    run, and the library refuses to launch it.  Here the build fails, and says why."""
+    if os.path.basename(src) != "launch_attention.cu":
+        return
+    wanted = int(re.search(r"constexpr int kLaunchRegs = (\d+)", open(os.path.join(CSRC, "spechub_attention.cuh")).read()).group(1))
+    found = {name: n for name, n in registers_of(log).items() if "attention_kernel" in name}
+    if not found or any(n != wanted for n in found.values()):
+        raise RuntimeError("attention_kernel needs %d registers a thread (kLaunchRegs in spechub_attention.cuh, which goes with kSoftmaxRegs and "
+                           "kOtherRegs); this nvcc gives it %s" % (wanted, sorted(set(found.values())) or "none that it tells of"))
+
+
 def build_library(force: bool = False, verbose: bool = False) -> str:
     """Compile every .cu under csrc/ (in parallel) into one shared library; returns its path."""
     if not force and not is_stale():
@@ -52,8 +71,16 @@ def build_library(force: bool = False, verbose: bool = False) -> str:
         obj = os.path.join(obj_dir, os.path.basename(src) + ".o")
         if force or _older(obj, [src] + _headers()):
             tmp = obj + ".%d.tmp.o" % os.getpid()
-            subprocess.check_call([nvcc] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + [
-                "-I", INCLUDE, "-I", CSRC, "-c", "-o", tmp, src])
+            run = subprocess.run([nvcc] + NVCC_FLAGS + ["-Xptxas", "-v", "-I", INCLUDE, "-I", CSRC, "-c", "-o", tmp, src],
+                                 stderr=subprocess.PIPE, text=True)
+            told = re.compile(r"ptxas info|^\s+\d+ bytes stack frame")
+            sys.stderr.write("".join(x for x in run.stderr.splitlines(True) if verbose or not told.search(x)))
+            run.check_returncode()
+            try:
+                check_registers(src, run.stderr)
+            except RuntimeError:
+                os.remove(tmp)
+                raise
             os.replace(tmp, obj)
         return obj
 
