@@ -3,7 +3,7 @@
 // Mathematics.  A block of up to 256 rows (row = (sequence, node, query head of one cache head)) goes over its keys in tiles of
 // 128.  S = Q K^T; per row p = 2^(c s - r), l += sum p, O += P V, with c = scale log2(e) and r the row's reference, at first the
 // maximum of the first kStep keys.  Later maxima are not looked for: r is raised only where the weights of kStep keys sum up to more than
-// kMostSum (far from the end of every type here), to their maximum in whole steps, and O and l are scaled by 2^(r_old - r): the division
+// kMostSum (so no weight is larger than that, and all are numbers in fp16 too), to their maximum in whole steps, and O and l are scaled by 2^(r_old - r): the division
 // by l at the end makes the result the same.  Pieces of one row are joined by their references: out = sum_j 2^(r_j - R) O_j /
 // sum_j 2^(r_j - R) l_j.
 //
@@ -48,7 +48,10 @@ constexpr int kPieces = 4, kPieceReaders = 11;   // pieces that are known ahead;
 // Registers of a thread: what the block is launched with, and how its warpgroups share them then (a row of scores is 128).
 constexpr int kLaunchRegs = 168, kSoftmaxRegs = 200, kOtherRegs = 104;
 static_assert(256 * kSoftmaxRegs + 128 * kOtherRegs <= kAttThreads * kLaunchRegs, "the block's own registers");
-constexpr float kMostSum = 60000.f;   // of kStep weights, before the reference is raised: each of them is a number in fp16
+// What kStep weights may sum up to before the reference is raised.  None of them is negative, so none is larger than their sum, and all are
+// numbers in fp16, which ends at 65504.
+constexpr float kMostSum = 60000.f;
+static_assert(kMostSum < 65504.f, "weights of fp16 are numbers");
 // Scores that a thread has in registers at a time (32 / 64 / 128: 64 x 31 nodes behind 8192 shared tokens 370 / 339 / 348 us, 64 sequences of
 // 31 nodes 139 / 139 / 152).
 constexpr int kStep = 64;
