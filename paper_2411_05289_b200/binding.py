@@ -451,17 +451,25 @@ def spechub_verify_tree_static(target_logits, draft_logits, draft_tokens, unifor
 def spechub_tree_tables(tree: Tree, nodes: int, device="cuda"):
     """What the cache operators want to know of a tree of ``nodes`` nodes: dict(depth, mask).  ``depth`` int32
     [nodes] is a node's distance from the root, ``mask`` int32 [nodes][ceil(nodes / 32)] the nodes that it sees in
-    attention (its ancestors and itself) as bits.  A plan: made once per tree, on the host."""
+    attention (its ancestors and itself) as bits.  A plan: made once per tree, on the host.  Nodes come after their
+    parents, of which each has one at most; a ``child`` that says otherwise is refused (entries < 0 are no children, and what
+    a leaf's row says below its own number is not looked at)."""
     if nodes < 1:
         raise ValueError("a tree has at least one node")
     child = None if tree.child is None else tree.child.cpu().tolist()
     if child is not None and len(child) != nodes:
         raise ValueError("child must be [nodes][k]")
-    words, depth = (nodes + 31) // 32, [0] * nodes
+    leaf = None if child is None or tree.node_kind is None else tree.node_kind.cpu().tolist()
+    words, depth, parent = (nodes + 31) // 32, [0] * nodes, [-1] * nodes
     sees = [1 << n for n in range(nodes)]
     for n in range(nodes):
         for c in child[n] if child is not None else range(tree.k * n + 1, tree.k * n + 1 + tree.k):
+            if 0 <= c <= n and not (leaf and leaf[n]):
+                raise ValueError("node %d: child %d must be a later node" % (n, c))
             if n < c < nodes:
+                if parent[c] not in (-1, n):
+                    raise ValueError("node %d is a child of nodes %d and %d" % (c, parent[c], n))
+                parent[c] = n
                 depth[c] = depth[n] + 1
                 sees[c] |= sees[n]
     rows = [[((s >> (32 * w)) & 0xFFFFFFFF) - ((s >> (32 * w + 31) & 1) << 32) for w in range(words)] for s in sees]

@@ -279,3 +279,19 @@ def test_more_work_than_a_call_counts():
             args = dict(q=rows(d, gap, 1 << 30), out=rows(d, gap, 1 << 45), shared=FAKE, width=400000, shared_len=shared)
             assert attend(d, nbytes=0, **args) == (-7 if taken else -16), (taken, gap)
     assert "table" in sh.status_string(-16)
+
+
+def test_tables_refuse_what_is_no_tree_in_order():
+    make = lambda rows, kind=None: sh.Tree(levels=3, child=torch.tensor(rows, dtype=torch.int32),  # noqa: E731
+                                           node_kind=None if kind is None else torch.tensor(kind, dtype=torch.uint8))
+    none = [-1, -1]
+    for rows, word in (([[2, -1], none, [1, -1], none], "later"),          # node 1 comes before its parent
+                       ([[1, 2], [1, -1], none, none], "later"),           # ... is its own
+                       ([[1, 2], none, [0, -1], none], "later"),
+                       ([[1, 2], [3, -1], [3, -1], none], "child of nodes 1 and 2")):
+        with pytest.raises(ValueError, match=word):
+            sh.spechub_tree_tables(make(rows), 4, device="cpu")
+    # children behind the last node are none; both drafts may lead to one node; a leaf's row may hold anything that is not behind it
+    t = sh.spechub_tree_tables(make([[1, 2], [3, 3], [9, -1], [0, 0]], [0, 0, 0, 1]), 4, device="cpu")
+    np.testing.assert_array_equal(as_bits(t["mask"], 4)[:, :4], brute([-1, 0, 0, 1]))
+    assert t["depth"].tolist() == [0, 1, 1, 2]
