@@ -472,8 +472,9 @@ def spechub_tree_tables(tree: Tree, nodes: int, device="cuda"):
                 parent[c] = n
                 depth[c] = depth[n] + 1
                 sees[c] |= sees[n]
-    rows = [[((s >> (32 * w)) & 0xFFFFFFFF) - ((s >> (32 * w + 31) & 1) << 32) for w in range(words)] for s in sees]
-    return dict(depth=torch.tensor(depth, dtype=torch.int32).to(device), mask=torch.tensor(rows, dtype=torch.int32).to(device))
+    # (the words as bytes: a chain of 8000 nodes has two million of them)
+    mask = torch.frombuffer(bytearray().join(s.to_bytes(4 * words, "little") for s in sees), dtype=torch.int32).reshape(nodes, words)
+    return dict(depth=torch.tensor(depth, dtype=torch.int32).to(device), mask=mask.to(device))
 
 
 def spechub_cache_append(q, k, v, k_cache, v_cache, pages, lens, depth=None, inv_freq=None, pos_offset=0,

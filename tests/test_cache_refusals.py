@@ -295,3 +295,14 @@ def test_tables_refuse_what_is_no_tree_in_order():
     t = sh.spechub_tree_tables(make([[1, 2], [3, 3], [9, -1], [0, 0]], [0, 0, 0, 1]), 4, device="cpu")
     np.testing.assert_array_equal(as_bits(t["mask"], 4)[:, :4], brute([-1, 0, 0, 1]))
     assert t["depth"].tolist() == [0, 1, 1, 2]
+
+
+def test_tables_of_a_long_chain():
+    """A prompt's chunk: the mask is a triangle; made in bytes, not number by number."""
+    n = 4099
+    t = sh.spechub_tree_tables(sh.Tree(levels=n, k=1), n, device="cpu")
+    words = t["mask"].numpy().view(np.uint8)
+    assert t["mask"].shape == (n, 129) and t["mask"].dtype == torch.int32 and t["mask"].is_contiguous()
+    np.testing.assert_array_equal(np.unpackbits(words, axis=1, bitorder="little")[:, :n], np.tri(n, dtype=np.uint8))
+    assert not np.unpackbits(words, axis=1, bitorder="little")[:, n:].any()
+    assert t["depth"].tolist() == list(range(n))
