@@ -74,7 +74,7 @@ extern "C" {
 
 #define SPECHUB_ERR_ALIGN (-11)  /* a pointer or stride is not a multiple of 16 bytes, or rows overlap: see Overlaps */
 #define SPECHUB_ERR_CACHE (-12)  /* bad cache or head shape: see spechub_cache_desc */
-#define SPECHUB_ERR_ROTARY (-13) /* rotated is not a multiple of 16 from 0 to head_dim, or interleaved is not 0 / 1 */
+#define SPECHUB_ERR_ROTARY (-13) /* rotated is not a multiple of 16 from 0 to head_dim, interleaved is not 0 / 1, or |pos_offset| > 2^53 where rotated > 0 */
 #define SPECHUB_ERR_SHARED (-14) /* shared_len < 0, or more tokens than shared_width pages hold */
 #define SPECHUB_ERR_SCALE (-15)  /* scale is not > 0, or scale * log2(e) is no finite number */
 #define SPECHUB_ERR_WORK (-16)   /* more work than one call of spechub_tree_attention counts: see there */
@@ -121,7 +121,8 @@ typedef struct spechub_heads {
  *   (x0 cos a - x1 sin a, x0 sin a + x1 cos a) with a = p * inv_freq[i],
  *   i < rotated / 2; a pair is (i, i + rotated / 2), or (2i, 2i + 1) if
  *   `interleaved`.  The angle is formed in 64 bits (far positions lose their
- *   turns' fraction in 32) and the result rounded once.
+ *   turns' fraction in 32) and the result rounded once.  The angle is off by
+ *   2^-51 of itself at most, less than 2^-20 at 2^31 with an inv_freq of 1.
  *   k goes to slot lens[b] + n of k_cache, v unchanged to v_cache, rotated q
  *   to q_out; q_out may be q itself.  q may be NULL (then q_out is not looked
  *   at), and inv_freq where rotated = 0.

@@ -25,6 +25,7 @@ int check_cache_desc(const spechub_cache_desc *d) {
 }
 
 constexpr int64_t kMaxShared = 0x3fffffff;
+constexpr int64_t kMostOffset = 1ll << 53;   // positions are whole numbers in 64-bit floating point up to here
 
 bool at16(const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
@@ -165,6 +166,7 @@ int spechub_cache_append(const spechub_cache_desc *desc, const spechub_heads *q,
     if (rc != SPECHUB_OK) return rc;
     if (desc->layers != 1) return SPECHUB_ERR_CACHE;
     if (rotated < 0 || rotated > desc->head_dim || rotated % 16 != 0 || (interleaved != 0 && interleaved != 1)) return SPECHUB_ERR_ROTARY;
+    if (rotated > 0 && (pos_offset > kMostOffset || pos_offset < -kMostOffset)) return SPECHUB_ERR_ROTARY;
     if (depth_stride_seq < 0 || (depth_stride_seq != 0 && depth_stride_seq < desc->nodes)) return SPECHUB_ERR_STRIDE;
     if (desc->batch == 0) return SPECHUB_OK;
     AppendArgs a = {};

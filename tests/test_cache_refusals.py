@@ -306,3 +306,11 @@ def test_tables_of_a_long_chain():
     np.testing.assert_array_equal(np.unpackbits(words, axis=1, bitorder="little")[:, :n], np.tri(n, dtype=np.uint8))
     assert not np.unpackbits(words, axis=1, bitorder="little")[:, n:].any()
     assert t["depth"].tolist() == list(range(n))
+
+
+def test_positions_that_64_bits_do_not_hold():
+    for offset in ((1 << 53) + 1, -(1 << 53) - 1, (1 << 63) - 1, -(1 << 63)):
+        assert append(offset=offset) == -13, offset
+        assert append(offset=offset, rotated=0, qo=heads(head=128)) == -11    # (nothing is rotated; the next check)
+    assert append(offset=1 << 53, qo=heads(head=128)) == -11 and append(offset=-(1 << 53), qo=heads(head=128)) == -11
+    assert "pos_offset" in sh.status_string(-13)
