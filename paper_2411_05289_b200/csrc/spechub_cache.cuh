@@ -157,7 +157,7 @@ __global__ void __launch_bounds__(kAcceptThreads) accept_kernel(const __grid_con
         if (s_end) break;
     }
     if (blockIdx.y == 0 && tid == 0) {
-        A.lens_out[b] = static_cast<int32_t>(len + kept);
+        A.lens_out[b] = static_cast<int32_t>(min(len + kept, int64_t(0x7fffffff)));   // (not the length of an absent sequence)
         if (c.status) c.status[b] = st;
     }
 }

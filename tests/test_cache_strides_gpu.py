@@ -1,7 +1,8 @@
-"""The cache operators' strides: tensors whose strides do not nest, and tensors that lie over themselves."""
+"""The cache operators' strides and lengths at their limits: tensors whose strides do not nest, that lie over themselves or between
+each other; the largest length."""
 import pytest
 
-from test_cache_gpu import Case, sh, tree_mask  # noqa: F401  (sh: the fixture)
+from test_cache_gpu import Case, make_cache, sh, tree_mask  # noqa: F401  (sh: the fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -95,3 +96,16 @@ def test_accept_of_keys_and_values_in_one_tensor(sh):
     with pytest.raises(sh.SpecHubError) as e:
         sh.spechub_cache_accept(kv, kv, table, lens, path, 7)
     assert e.value.code == -11
+
+
+def test_accept_at_the_largest_length(sh):
+    """Far behind the table: nothing moves, and the sequence does not become one that is absent."""
+    gen = torch.Generator(device="cuda").manual_seed(7)
+    kc, vc = make_cache(gen, 4, 8, 1, 64, torch.bfloat16)
+    old = kc.clone(), vc.clone()
+    lens = torch.tensor([2147483647, 2147483646, 2147483640], dtype=torch.int32, device="cuda")
+    table = torch.arange(4, dtype=torch.int32, device="cuda")[None].expand(3, 4).contiguous()
+    path = torch.tensor([[0, 2, 6]] * 3, dtype=torch.int32, device="cuda")
+    got = sh.spechub_cache_accept(kc, vc, table, lens, path, 7)
+    assert got["lens"].tolist() == [2147483647, 2147483647, 2147483643] and got["status"].tolist() == [128] * 3
+    assert torch.equal(kc, old[0]) and torch.equal(vc, old[1])
