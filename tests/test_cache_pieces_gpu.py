@@ -1,5 +1,7 @@
 """Tree attention: blocks that several CTAs share, and blocks that one CTA finishes, in one CTA's run.  Values and tolerances
 as in test_cache_gpu.py."""
+import gc
+
 import pytest
 
 from test_cache_gpu import Case, sh, tree_mask  # noqa: F401  (sh: the fixture)
@@ -7,6 +9,14 @@ from test_cache_gpu import Case, sh, tree_mask  # noqa: F401  (sh: the fixture)
 pytestmark = pytest.mark.gpu
 
 torch = pytest.importorskip("torch")
+
+
+@pytest.fixture(scope="module", autouse=True)
+def nothing_left():
+    """The modules behind this one find the device's memory as it was: frames that an exception's traceback keeps alive go, too."""
+    yield
+    gc.collect()
+    torch.cuda.empty_cache()
 
 
 @pytest.mark.parametrize("dt", ["bf16", "fp16"])

@@ -1,5 +1,7 @@
 """The cache operators' strides and lengths at their limits: tensors whose strides do not nest, that lie over themselves or between
 each other; the largest length."""
+import gc
+
 import pytest
 
 from test_cache_gpu import Case, make_cache, sh, tree_mask  # noqa: F401  (sh: the fixture)
@@ -7,6 +9,14 @@ from test_cache_gpu import Case, make_cache, sh, tree_mask  # noqa: F401  (sh: t
 pytestmark = pytest.mark.gpu
 
 torch = pytest.importorskip("torch")
+
+
+@pytest.fixture(scope="module", autouse=True)
+def nothing_left():
+    """The modules behind this one find the device's memory as it was: frames that an exception's traceback keeps alive go, too."""
+    yield
+    gc.collect()
+    torch.cuda.empty_cache()
 
 
 def test_outputs_whose_strides_do_not_nest(sh):
