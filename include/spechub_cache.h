@@ -148,7 +148,8 @@ int spechub_cache_append(const spechub_cache_desc *desc, const spechub_heads *q,
  *   A key or value that is NaN or infinite concerns the rows that see it only.
  *   Scores, sums and the output before its one rounding are held in 32 bits;
  * the weights are rounded to the cache's type for their product with the
- * values.  The result does not depend on when which block runs: the same call
+ * values.  Scores (scale * q . k) are up to 2^25 in magnitude; where they are
+ * larger, 32 bits hold them to whole numbers only, and a row may lose its weights.  The result does not depend on when which block runs: the same call
  * on the same GPU model gives the same bits.
  *   workspace: device scratch, 16-byte aligned, of at least
  * spechub_tree_attention_workspace_bytes(desc, shared_len) bytes.  It need not

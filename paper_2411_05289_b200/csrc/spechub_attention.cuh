@@ -6,6 +6,10 @@
 // kMostSum (so no weight is larger than that, and all are numbers in fp16 too), to their maximum in whole steps, and O and l are scaled by 2^(r_old - r): the division
 // by l at the end makes the result the same.  Pieces of one row are joined by their references: out = sum_j 2^(r_j - R) O_j /
 // sum_j 2^(r_j - R) l_j.
+//   S, r, l, O and all that joins them are 32 bits.  P is rounded once to the cache's type, because the tensor core takes P and V in one 16-bit
+// type; P in two terms of 16 bits would keep 32 bits' worth and double the product.  l adds the weights before that rounding.  Against 64
+// bits out is then off by 0.0021 to 0.0023 in relation in bf16 and 0.00029 in fp16, where weights in 32 bits leave the 0.0017 and 0.00021 of out's own
+// rounding.
 //
 // Work.  Rows that share keys are one block: the query heads of a cache head and all nodes of a sequence for its own context (7
 // nodes of 4 heads are 28 rows), and the whole batch for the shared prefix, which is thus read once per 256 rows, from L2 but for the
@@ -30,9 +34,10 @@
 // 0 * NaN would reach every row; the rows that do see such a node get it added at the end.
 //
 // What bounds it, measured on inputs larger than L2: few rows, memory (64 sequences of one node, 1000 to 8192 tokens of 8 heads of 128:
-// 201 us, 6.0 TB/s); many rows, the chain scores, weights, product of two groups, with the tensor cores and the special-function units
-// busy half of the time each (64 x 31 nodes of 32 heads, 8192 tokens shared and 100 to 1000 own: 336 us, 845 TFLOP/s); short contexts,
-// the 3 us between pieces.  In loops of seconds the power limit holds the first two at 223 and 371 us.
+// 205 us, 5.9 TB/s); many rows, the chain scores, weights, product of two groups, with the tensor cores and the special-function units
+// busy half of the time each (64 x 31 nodes of 32 heads, 8192 tokens shared and 100 to 1000 own: 345 us, 823 TFLOP/s); short contexts,
+// the 3 us between pieces.  In loops of seconds the power limit holds the first two at 221 and 369 us.  (What other comments here compare was
+// measured side by side when the choice was made; both sides have become faster since.)
 #pragma once
 
 #include "spechub_pages.cuh"
@@ -411,7 +416,7 @@ __global__ void __launch_bounds__(kAttThreads, 1) attention_kernel(const __grid_
         tma_prefetch_map(&maps.q);
     }
     // The tensor core multiplies rows that are not there too, and what long runs of calls take goes by the power limit: such rows of the
-    // queries and of the weights are zeros (64 sequences of one node 261 -> 236 us, two of 15 nodes 206 -> 199).
+    // queries and of the weights are zeros (64 sequences of one node 261 -> 233 us, two of 15 nodes 206 -> 199, in loops of seconds).
     for (int i = tid; i < 2 * L::kTileBytes / 16; i += kAttThreads) st_shared(s_q + 16 * i, 0, 0, 0, 0);
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     pdl_begin();
