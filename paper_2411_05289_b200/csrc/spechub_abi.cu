@@ -639,7 +639,7 @@ const char *spechub_status_string(int code) {
         case SPECHUB_ERR_WORKSPACE: return "workspace smaller than spechub_workspace_bytes()";
         case SPECHUB_ERR_LAUNCH: return "kernel launch failed";
         case SPECHUB_ERR_METHOD: return "without_replacement must be 0 or 1";
-        case SPECHUB_ERR_ALIGN: return "pointers and strides must be multiples of 16 bytes, rows that are written apart from each other";
+        case SPECHUB_ERR_ALIGN: return "pointers and strides must be multiples of 16 bytes, rows that are written apart from each other and from what the call reads elsewhere (q_out may be q)";
         case SPECHUB_ERR_CACHE: return "bad cache: need heads a multiple of kv_heads >= 1 (attention: at most 128 times), head_dim 64 or 128, page_size a power of two from 8 to 1024, pages >= 1, table_width >= 1, layers >= 1 (1 but for accept)";
         case SPECHUB_ERR_ROTARY: return "rotated must be a multiple of 16 from 0 to head_dim, interleaved 0 or 1, pos_offset from -2^53 to 2^53";
         case SPECHUB_ERR_SHARED: return "shared_len must be >= 0 and fit into the shared pages";
