@@ -494,8 +494,8 @@ def spechub_tree_attention(q, k_cache, v_cache, pages, lens, mask, scale=None, s
     """Attention of every node to the ``shared_len`` tokens of ``shared_pages`` (int32, a prefix that the whole batch
     shares: read once for all), to its sequence's own context and to the nodes that it sees (``mask`` from
     ``spechub_tree_tables``, or one per sequence).  ``scale`` defaults to head_dim ** -0.5.  Pass ``out`` (a dict that a
-    former call returned) to reuse its tensors; rows of absent sequences are left as they were.  Returns dict(out, lse,
-    status)."""
+    former call returned) to reuse its tensors, which share no element with q; rows of absent sequences are left as they were.
+    Returns dict(out, lse, status)."""
     return (_native or _load_native()).tree_attention(q, k_cache, v_cache, pages, lens, mask, scale, shared_pages,
                                                       shared_len, out, stream)
 

@@ -119,3 +119,34 @@ def test_accept_at_the_largest_length(sh):
     got = sh.spechub_cache_accept(kc, vc, table, lens, path, 7)
     assert got["lens"].tolist() == [2147483647, 2147483647, 2147483643] and got["status"].tolist() == [128] * 3
     assert torch.equal(kc, old[0]) and torch.equal(vc, old[1])
+
+
+@pytest.mark.parametrize("dt", ["bf16", "fp16"])
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("d,shared,n", [(64, 0, 1), (128, 200, 33)])
+def test_scores_of_the_largest_magnitude(sh, d, shared, n, sign, dt):
+    """Scores of 2^25, exact in 32 bits, at every third key and below it by 2^18 at the others: all weight is at those keys.
+    Their weights are equal, whatever the reference is rounded to: out is their values' mean, off by the common rounding of the weights and its
+    own (2 u |out|) and by the sums' (n 2^-23 of the values); lse by half the spacing of 2^26 twice, the second time by ln 2."""
+    c = Case(23, [500, 3, 260], n, 1, 4, d, 16, dt, shared=shared, mask=tree_mask(n), q_sd=0.0)
+    c.q[..., 0] = 4096.0
+    for pages, count in [(c.ids_shared, shared)] + [(c.table[i], x + n) for i, x in enumerate(c.lens_list)]:
+        for at in range(count):
+            key = c.kc[int(pages[at // 16]), at % 16]
+            key[:] = 0
+            key[..., 0] = sign * 8192.0 if at % 3 == 0 else sign * 8192.0 - 64.0
+    got = c.run(sh, scale=1.0)
+    assert got["status"].tolist() == [0, 0, 0]
+    u = torch.finfo(c.dt).eps / 2
+    for i, x in enumerate(c.lens_list):
+        k = torch.cat((c.flat(c.kc, c.ids_shared, shared), c.flat(c.kc, c.table[i], x + n)))[:, 0, 0]
+        v = torch.cat((c.flat(c.vc, c.ids_shared, shared), c.flat(c.vc, c.table[i], x + n)))[:, 0]
+        sees = torch.ones((n, len(k)), dtype=torch.bool, device="cuda")
+        sees[:, shared + x:] = torch.from_numpy(c.sees).cuda()
+        top = torch.where(sees, k, -1e9).amax(1)
+        hit = (sees & (k == top[:, None])).double()
+        want = hit @ v / hit.sum(1, keepdim=True)
+        far = (got["out"][i].double() - want[:, None]).abs()
+        assert bool((far <= 2 * u * want[:, None].abs() + len(k) * 2.0 ** -23 * v.abs().max() + (2.0 ** -25 if dt == "fp16" else 0)).all())
+        lse = top * 4096 + hit.sum(1).log()
+        assert bool(((got["lse"][i].double() - lse[:, None]).abs() <= 2 + 2 * 0.7).all())
